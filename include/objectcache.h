@@ -261,6 +261,144 @@ int oc_rest_of_layer(const void *attn_out, int64_t tokens, const oc_layout *layo
                      void *stream);
 
 /* ---------------------------------------------------------------------------
+ * The prefix held in 4 bits.  A 4-bit pool is an oc_kv_pool whose base points
+ * to oc_kv4_pool_bytes() of device memory laid out [L][2][P][page]: per layer
+ * K's pages, then V's.  A page holds, for each KV head and slot, d/2 bytes of
+ * codes (two to a byte, the even dimension in the low half), then for each head
+ * and slot d/32 scale bytes, then zero to 15 bytes that nothing reads, up to a
+ * multiple of 16.  A code is a sign bit over three bits that stand for
+ * 0 0.5 1 1.5 2 3 4 6; 32 consecutive dimensions share a scale byte b, and a
+ * value is its code times 2^(b - 127); b = 255 makes all 32 NaN.
+ *
+ * A block of 32 is stored as follows: 2^(b - 127) is the least power of two of
+ * which seven cover the block's largest magnitude, b held to 2..252; every value
+ * over it is rounded to the nearest code, ties to the even one, magnitudes past
+ * 6 to 6; a zero keeps its sign.  A block that holds an infinity or a NaN gets
+ * b = 255 and codes of 0.  The stored bytes are thus defined to the bit.
+ *
+ * These entry points take the layouts of the bfloat16 ones where head_dim is
+ * a multiple of 32 (attention: 64 or 128, with a page_size of 16); their checks,
+ * errors and streams are those of the entry points they are named after.
+ * Positions are 32-bit: 2^31 tokens or more are OC_ERANGE.
+ * ------------------------------------------------------------------------- */
+
+/* Bytes of a 4-bit pool of this layout (0: the layout is not supported). */
+size_t oc_kv4_pool_bytes(const oc_layout *layout);
+
+/* oc_kv_layer_ingest into a 4-bit pool: the bfloat16 payload of one layer is
+ * quantised into the pages of the block table.  Slots past the prefix are not
+ * written. */
+int oc_kv4_layer_ingest(const oc_staging *staging, const oc_block_table *block_table, oc_kv_pool *kv_pool,
+                        int32_t layer, void *stream);
+
+/* oc_kv_suffix_append into a 4-bit pool. */
+int oc_kv4_suffix_append(const void *k_new, const void *v_new, int64_t suffix_tokens,
+                         const oc_block_table *block_table, oc_kv_pool *kv_pool, int32_t layer, void *stream);
+
+/* oc_kv_layer_gather out of a 4-bit pool: the payload receives the bfloat16
+ * values that the codes stand for, exactly (b = 0 and 1 give subnormals, which
+ * are kept; magnitudes past bfloat16's range, which no stored block has, become
+ * infinities). */
+int oc_kv4_layer_gather(const oc_block_table *block_table, const oc_kv_pool *kv_pool, int32_t layer,
+                        void *staging_out, int64_t num_chunks, int64_t per_layer_chunk_bytes, void *stream);
+
+/* Bytes of device workspace oc_kv4_suffix_prefill_layer needs for these lengths
+ * (at least 256; 0 means the layout or lengths are not supported). */
+size_t oc_kv4_attention_workspace_bytes(const oc_layout *layout, int64_t prefix_tokens, int64_t suffix_tokens);
+
+/* oc_suffix_prefill_layer over a prefix held in 4 bits: the prefix's K and V
+ * are the values that its codes stand for (exact in bfloat16), the suffix's are
+ * k_new and v_new as they are.  Same arguments, workspace rules, rounding and
+ * asynchrony.  An infinity or NaN in a k_new or v_new row reaches no row of a
+ * token before it. */
+int oc_kv4_suffix_prefill_layer(const void *q, const void *k_new, const void *v_new, int64_t suffix_tokens,
+                                const oc_kv_pool *kv_pool, const oc_block_table *block_table, int32_t layer,
+                                void *out, void *workspace, size_t workspace_bytes, void *stream);
+
+/* Several block tables in one device array of int32 page ids: table i begins at
+ * pages + i * stride and has num_entries entries.  With more than one table
+ * stride >= num_entries. */
+typedef struct {
+    int32_t *pages;
+    int64_t num_tables;
+    int64_t num_entries;
+    int64_t stride;
+} oc_page_tables;
+
+/* Bytes of device workspace oc_kv4_decode_layer needs (at least 256; 0 means
+ * that the layout or sizes are not supported). */
+size_t oc_kv4_decode_workspace_bytes(const oc_layout *layout, int64_t batch, int64_t max_tokens);
+
+/* One new token for each of `batch` requests, over their prefixes in a 4-bit
+ * pool: request i's row attends to its num_tokens[i] cached tokens and to
+ * itself (from k_new / v_new, as they are), and its K and V are appended, in 4
+ * bits, at position num_tokens[i].
+ * q, out: device [batch][n_q][d]; k_new, v_new: device [batch][n_kv][d];
+ * bfloat16, 16-byte aligned.  num_tokens is DEVICE int32 [batch]: a captured
+ * call can be replayed as the requests grow; the caller adds 1 after the last
+ * layer.  num_tokens[i] < 0 marks an empty place: nothing of it is read or
+ * written.  Lengths above max_tokens are taken as max_tokens.  Every table needs
+ * max_tokens / page_size + 1 entries, of which the first
+ * num_tokens[i] / page_size + 1 are used; the page that receives the token must
+ * be no other table's (oc_kv_pages_fork sees to that).  batch == 0 is not an
+ * error; batch <= 65535.  workspace: device, at least
+ * oc_kv4_decode_workspace_bytes(), 256-byte aligned.  Asynchronous on
+ * `stream`. */
+int oc_kv4_decode_layer(const void *q, const void *k_new, const void *v_new, int64_t batch, oc_kv_pool *kv_pool,
+                        const oc_page_tables *tables, const int32_t *num_tokens, int64_t max_tokens, int32_t layer,
+                        void *out, void *workspace, size_t workspace_bytes, void *stream);
+
+/* ---------------------------------------------------------------------------
+ * Pages of a pool, of either kind (bits: 16 for bfloat16, 4 for 4-bit): forked
+ * between requests that share a prefix, copied, freed and moved together.  The
+ * state is page_counts, DEVICE int32 [P], caller-owned: how many tables hold
+ * each page; a page whose count is not positive is free.  Everything happens
+ * on the device in the order of `stream`; what only the device can find out, that
+ * no page is left, goes to a device int32 `status` (OC_OK or OC_ENOMEM).
+ * Calls that share page_counts must be ordered.  Page ids outside [0, P) in
+ * device tables are left out.
+ * ------------------------------------------------------------------------- */
+
+/* The n lowest free pages, ascending, to device pages_out[0..n), each with a
+ * count of 1.  With fewer than n free pages *status is OC_ENOMEM, pages_out is -1
+ * throughout, and the counts stay as they were. */
+int oc_kv_pages_take(const oc_layout *layout, int32_t *page_counts, int64_t n, int32_t *pages_out, int32_t *status,
+                     void *stream);
+
+/* Copy page src_pages[i] to page dst_pages[i], K and V of every layer, for
+ * i < n (device arrays, n <= P).  The dst ids must be distinct and none of
+ * them may be among the src ids; a source may repeat.  n == 0 is not an error. */
+int oc_kv_pages_copy(oc_kv_pool *kv_pool, int32_t bits, const int32_t *src_pages, const int32_t *dst_pages, int64_t n,
+                     void *stream);
+
+/* Fork a request into num_children more that start from its num_tokens tokens.
+ * Table c of `children` receives ceil(num_tokens / page_size) entries: the
+ * parent's whole pages, shared (their counts grow by num_children), and, where
+ * the last page is partly filled, a page of the child's own (the lowest free
+ * ones, ascending by child, with a count of 1) into which all of the parent's is
+ * copied, so that each may append to its own.  With too few free pages *status is
+ * OC_ENOMEM, the children's last entries are -1, and nothing else changes. */
+int oc_kv_pages_fork(oc_kv_pool *kv_pool, int32_t bits, const oc_block_table *parent, const oc_page_tables *children,
+                     int64_t num_children, int32_t *page_counts, int32_t *status, void *stream);
+
+/* A request ends: the counts of its table's ceil(num_tokens / page_size) pages
+ * fall by 1; those that reach 0 are free.  Pages keep their contents. */
+int oc_kv_pages_release(const oc_block_table *block_table, const oc_layout *layout, int32_t *page_counts, void *stream);
+
+/* Bytes of device workspace oc_kv_pages_compact needs (0: unsupported). */
+size_t oc_kv_pages_workspace_bytes(const oc_layout *layout);
+
+/* Move the held pages to the front of the pool: with n of them held, the ones at
+ * n and behind go, in ascending order, to the free pages before n, in ascending
+ * order; K and V of every layer, counts included.  Every entry of `tables` that
+ * names a moved page is rewritten (entries outside [0, P) are left alone, so
+ * tables may be longer than their requests).  *num_live (device int32) = n.
+ * workspace: device, 16-byte aligned, at least oc_kv_pages_workspace_bytes();
+ * it need not start at zero. */
+int oc_kv_pages_compact(oc_kv_pool *kv_pool, int32_t bits, int32_t *page_counts, const oc_page_tables *tables,
+                        int32_t *num_live, void *workspace, size_t workspace_bytes, void *stream);
+
+/* ---------------------------------------------------------------------------
  * Layerwise pipeline (Section 3.5, eq. (3)): for every layer, the payload
  * lands (host producer -> pinned slot -> DMA into an HBM slot), is ingested
  * into the pool, and the layer's attention runs on a second stream as soon

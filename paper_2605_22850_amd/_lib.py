@@ -32,7 +32,10 @@ EXPORTS = [
     "oc_kv_layer_gather", "oc_kv_chunks_gather", "oc_kv_suffix_append", "oc_rest_of_layer",
     "oc_attention_workspace_bytes", "oc_suffix_prefill_layer", "oc_context_create", "oc_pipeline_run",
     "oc_pipeline_last_ms", "oc_context_destroy", "oc_bandwidth_allocate", "oc_suffix_prefill_layer_noalloc",
-    "oc_epoch_schedule",
+    "oc_epoch_schedule", "oc_kv4_pool_bytes", "oc_kv4_layer_ingest", "oc_kv4_suffix_append", "oc_kv4_layer_gather",
+    "oc_kv4_attention_workspace_bytes", "oc_kv4_suffix_prefill_layer", "oc_kv4_decode_workspace_bytes",
+    "oc_kv4_decode_layer", "oc_kv_pages_take", "oc_kv_pages_copy", "oc_kv_pages_fork", "oc_kv_pages_release",
+    "oc_kv_pages_workspace_bytes", "oc_kv_pages_compact",
 ]
 OC_NOALLOC_WORKSPACE_BYTES = 65 << 20
 
@@ -79,6 +82,10 @@ class c_layer_buffers(ctypes.Structure):
     _fields_ = [("o", c_void_p), ("gate_up", c_void_p), ("act", c_void_p), ("h", c_void_p), ("qkv", c_void_p)]
 
 
+class c_page_tables(ctypes.Structure):
+    _fields_ = [("pages", c_void_p), ("num_tables", c_int64), ("num_entries", c_int64), ("stride", c_int64)]
+
+
 class c_request(ctypes.Structure):
     _fields_ = [("prefix_tokens", c_int64), ("suffix_tokens", c_int64), ("block_table", POINTER(c_block_table)),
                 ("chunk_objects", POINTER(c_void_p)), ("device_payload", c_void_p), ("q", c_void_p),
@@ -98,6 +105,10 @@ _fast = None
 # the library's functions behind _marshal's, in the order its bind() takes them
 _FAST = ["oc_kv_layer_ingest", "oc_kv_chunks_ingest", "oc_kv_layer_gather", "oc_kv_chunks_gather",
          "oc_kv_suffix_append", "oc_suffix_prefill_layer", "oc_suffix_prefill_layer_noalloc", "oc_rest_of_layer"]
+# those of the 4-bit cache and of the page operations, in the order bind_kv4() takes them
+_FAST_KV4 = ["oc_kv4_layer_ingest", "oc_kv4_suffix_append", "oc_kv4_layer_gather", "oc_kv4_suffix_prefill_layer",
+             "oc_kv4_decode_layer", "oc_kv_pages_take", "oc_kv_pages_copy", "oc_kv_pages_fork", "oc_kv_pages_release",
+             "oc_kv_pages_compact"]
 
 
 def _native():
@@ -114,6 +125,7 @@ def _native():
         m = module_from_spec(spec)
         spec.loader.exec_module(m)
         m.bind(_current_stream, *(ctypes.cast(getattr(L, f), c_void_p).value for f in _FAST))
+        m.bind_kv4(*(ctypes.cast(getattr(L, f), c_void_p).value for f in _FAST_KV4))
         _fast = m
     return _fast
 
@@ -169,6 +181,29 @@ def lib():
         L.oc_epoch_schedule.argtypes = [c_int32, c_int32, POINTER(c_double), POINTER(c_double), c_int32,
                                         POINTER(c_double), c_double, c_double, c_double, POINTER(c_double),
                                         POINTER(c_double)]
+        PT = POINTER(c_page_tables)
+        L.oc_kv4_layer_ingest.argtypes = L.oc_kv_layer_ingest.argtypes
+        L.oc_kv4_suffix_append.argtypes = L.oc_kv_suffix_append.argtypes
+        L.oc_kv4_layer_gather.argtypes = L.oc_kv_layer_gather.argtypes
+        L.oc_kv4_suffix_prefill_layer.argtypes = L.oc_suffix_prefill_layer.argtypes
+        L.oc_kv4_decode_layer.argtypes = [c_void_p, c_void_p, c_void_p, c_int64, POINTER(c_kv_pool), PT, c_void_p,
+                                          c_int64, c_int32, c_void_p, c_void_p, c_size_t, c_void_p]
+        L.oc_kv_pages_take.argtypes = [POINTER(c_layout), c_void_p, c_int64, c_void_p, c_void_p, c_void_p]
+        L.oc_kv_pages_copy.argtypes = [POINTER(c_kv_pool), c_int32, c_void_p, c_void_p, c_int64, c_void_p]
+        L.oc_kv_pages_fork.argtypes = [POINTER(c_kv_pool), c_int32, POINTER(c_block_table), PT, c_int64, c_void_p,
+                                       c_void_p, c_void_p]
+        L.oc_kv_pages_release.argtypes = [POINTER(c_block_table), POINTER(c_layout), c_void_p, c_void_p]
+        L.oc_kv_pages_compact.argtypes = [POINTER(c_kv_pool), c_int32, c_void_p, PT, c_void_p, c_void_p, c_size_t,
+                                          c_void_p]
+        L.oc_kv4_attention_workspace_bytes.argtypes = [POINTER(c_layout), c_int64, c_int64]
+        L.oc_kv4_decode_workspace_bytes.argtypes = [POINTER(c_layout), c_int64, c_int64]
+        for name in ("oc_kv4_pool_bytes", "oc_kv_pages_workspace_bytes"):
+            getattr(L, name).argtypes = [POINTER(c_layout)]
+        for name in ("oc_kv4_pool_bytes", "oc_kv_pages_workspace_bytes", "oc_kv4_attention_workspace_bytes",
+                     "oc_kv4_decode_workspace_bytes"):
+            getattr(L, name).restype = c_size_t
+        for name in _FAST_KV4:
+            getattr(L, name).restype = c_int
         for name in ("oc_block_table_check", "oc_kv_layer_ingest", "oc_kv_chunks_ingest", "oc_kv_layer_gather",
                      "oc_kv_chunks_gather", "oc_kv_suffix_append", "oc_rest_of_layer", "oc_suffix_prefill_layer",
                      "oc_suffix_prefill_layer_noalloc", "oc_bandwidth_allocate", "oc_epoch_schedule"):
@@ -300,6 +335,101 @@ def oc_suffix_prefill_layer_noalloc(q, k_new, v_new, suffix_tokens: int, pool, l
     static per-device workspace holds the split partials."""
     _check(_native().suffix_prefill_layer_noalloc(q, k_new, v_new, suffix_tokens, pool, layout, pages, num_tokens,
                                                   layer, out, stream))
+
+
+# ---------------------------------------------------------------------------
+# the prefix held in 4 bits
+# ---------------------------------------------------------------------------
+
+def _bytes_of(name: str, layout: Layout, *sizes: int) -> int:
+    lay = layout.c()
+    n = getattr(lib(), name)(ctypes.byref(lay), *sizes)
+    if n == 0:
+        raise OcError(OC_EINVAL, lib().oc_last_error().decode() or "unsupported shape")
+    return n
+
+
+def oc_kv4_pool_bytes(layout: Layout) -> int:
+    """Bytes of a 4-bit pool: allocate it as a uint8 tensor of that many elements."""
+    return _bytes_of("oc_kv4_pool_bytes", layout)
+
+
+def oc_kv4_layer_ingest(staging, num_chunks: int, pages, num_tokens: int, pool, layout: Layout, layer: int,
+                        stream=None) -> None:
+    """One layer's bfloat16 payload, quantised into the pages of a 4-bit pool."""
+    _check(_native().kv4_layer_ingest(staging, num_chunks, pages, num_tokens, pool, layout, layer, stream))
+
+
+def oc_kv4_suffix_append(k_new, v_new, suffix_tokens: int, pages, num_tokens: int, pool, layout: Layout,
+                         layer: int, stream=None) -> None:
+    """One layer's suffix K/V, quantised to the positions num_tokens .. of a 4-bit pool."""
+    _check(_native().kv4_suffix_append(k_new, v_new, suffix_tokens, pages, num_tokens, pool, layout, layer, stream))
+
+
+def oc_kv4_layer_gather(pages, num_tokens: int, pool, layout: Layout, layer: int, staging_out, num_chunks: int,
+                        stream=None) -> None:
+    """The bfloat16 values of a layer's prefix out of a 4-bit pool, as a layer payload."""
+    _check(_native().kv4_layer_gather(pages, num_tokens, pool, layout, layer, staging_out, num_chunks, stream))
+
+
+def oc_kv4_attention_workspace_bytes(layout: Layout, prefix_tokens: int, suffix_tokens: int) -> int:
+    return _bytes_of("oc_kv4_attention_workspace_bytes", layout, prefix_tokens, suffix_tokens)
+
+
+def oc_kv4_suffix_prefill_layer(q, k_new, v_new, suffix_tokens: int, pool, layout: Layout, pages, num_tokens: int,
+                                layer: int, out, workspace, stream=None) -> None:
+    """oc_suffix_prefill_layer over a prefix held in 4 bits."""
+    _check(_native().kv4_suffix_prefill_layer(q, k_new, v_new, suffix_tokens, pool, layout, pages, num_tokens, layer,
+                                              out, workspace, stream))
+
+
+def oc_kv4_decode_workspace_bytes(layout: Layout, batch: int, max_tokens: int) -> int:
+    return _bytes_of("oc_kv4_decode_workspace_bytes", layout, batch, max_tokens)
+
+
+def oc_kv4_decode_layer(q, k_new, v_new, batch: int, pool, layout: Layout, tables, num_tokens, max_tokens: int,
+                        layer: int, out, workspace, stream=None) -> None:
+    """One new token for each request: attention over its 4-bit prefix and itself, and its append.
+    `tables` is a 2-D int32 tensor, a row for each request; `num_tokens` device int32 [batch], negative for
+    an empty place."""
+    _check(_native().kv4_decode_layer(q, k_new, v_new, batch, pool, layout, tables, num_tokens, max_tokens, layer,
+                                      out, workspace, stream))
+
+
+# ---------------------------------------------------------------------------
+# pages of a pool (bits: 16 or 4)
+# ---------------------------------------------------------------------------
+
+def oc_kv_pages_take(page_counts, layout: Layout, n: int, pages_out, status, stream=None) -> None:
+    """The n lowest free pages (device int32 pages_out), each with a count of 1; OC_ENOMEM in `status` without."""
+    _check(_native().kv_pages_take(page_counts, layout, n, pages_out, status, stream))
+
+
+def oc_kv_pages_copy(pool, layout: Layout, bits: int, src_pages, dst_pages, n: int, stream=None) -> None:
+    """Pages src_pages[i] -> dst_pages[i], K and V of every layer (device int32 ids)."""
+    _check(_native().kv_pages_copy(pool, layout, bits, src_pages, dst_pages, n, stream))
+
+
+def oc_kv_pages_fork(pool, layout: Layout, bits: int, pages, num_tokens: int, num_children: int, child_tables,
+                     page_counts, status, stream=None) -> None:
+    """Fork a request: whole pages shared, the partial last one copied for each row of child_tables (2-D int32)."""
+    _check(_native().kv_pages_fork(pool, layout, bits, pages, num_tokens, num_children, child_tables, page_counts,
+                                   status, stream))
+
+
+def oc_kv_pages_release(pages, num_tokens: int, layout: Layout, page_counts, stream=None) -> None:
+    """A request ends: its pages' counts fall by one."""
+    _check(_native().kv_pages_release(pages, num_tokens, layout, page_counts, stream))
+
+
+def oc_kv_pages_workspace_bytes(layout: Layout) -> int:
+    return _bytes_of("oc_kv_pages_workspace_bytes", layout)
+
+
+def oc_kv_pages_compact(pool, layout: Layout, bits: int, page_counts, tables, num_live, workspace,
+                        stream=None) -> None:
+    """Held pages to the front of the pool; the entries of `tables` (2-D int32) follow them."""
+    _check(_native().kv_pages_compact(pool, layout, bits, page_counts, tables, num_live, workspace, stream))
 
 
 # ---------------------------------------------------------------------------

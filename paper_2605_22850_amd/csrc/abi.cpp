@@ -29,7 +29,7 @@ int check_copy_pieces(int64_t pieces, const char *what) {
     return OC_OK;
 }
 
-static int check_layout(const oc_layout &l) {
+int check_layout(const oc_layout &l) {
     if (l.num_layers < 1 || l.num_q_heads < 1 || l.num_kv_heads < 1 || l.head_dim < 1 || l.page_size < 1 ||
         l.chunk_tokens < 1 || l.num_pages < 1)
         return fail(OC_EINVAL, "layout fields must be positive");
@@ -39,7 +39,7 @@ static int check_layout(const oc_layout &l) {
     return OC_OK;
 }
 
-static int check_table(const oc_block_table *bt, const oc_layout &l) {
+int check_table(const oc_block_table *bt, const oc_layout &l) {
     if (!bt) return fail(OC_EINVAL, "block_table is NULL");
     if (bt->num_tokens < 0 || bt->num_entries < 0) return fail(OC_EINVAL, "negative block table size");
     const int64_t need = (bt->num_tokens + l.page_size - 1) / l.page_size;
@@ -112,8 +112,7 @@ int check_append_table(const oc_block_table *bt, const oc_layout &l, int64_t suf
     return OC_OK;
 }
 
-static int check_staging_shape(const oc_layout &l, const oc_block_table *bt, int64_t num_chunks,
-                               int64_t slice_bytes) {
+int check_staging_shape(const oc_layout &l, const oc_block_table *bt, int64_t num_chunks, int64_t slice_bytes) {
     const int64_t S = 2LL * l.chunk_tokens * l.num_kv_heads * l.head_dim * 2;
     if (num_chunks < 0) return fail(OC_EINVAL, "negative num_chunks");
     if (slice_bytes != S)

@@ -58,6 +58,12 @@ inline bool aligned(const void *p, uintptr_t a) { return (reinterpret_cast<uintp
 constexpr int64_t OC_MAX_GRID_ITEMS = 0xFFFFFFFFLL - 1023;
 int check_copy_pieces(int64_t pieces, const char *what);
 
+// Checks that the single-layer entry points share: the layout's fields, a
+// block table against it, and a payload's shape against both.
+int check_layout(const oc_layout &l);
+int check_table(const oc_block_table *bt, const oc_layout &l);
+int check_staging_shape(const oc_layout &l, const oc_block_table *bt, int64_t num_chunks, int64_t slice_bytes);
+
 // ---- ingest / gather ------------------------------------------------------
 struct IngestArgs {
     const uint16_t *staging;   // chunk slices [N][2][G][n_kv][d], chunk_stride apart
@@ -114,6 +120,26 @@ int check_append_table(const oc_block_table *bt, const oc_layout &l, int64_t suf
 // arguments for appending `suffix_tokens` tokens of `layer` behind bt->num_tokens
 AppendArgs append_args(const oc_kv_pool *pool, const oc_block_table *bt, int32_t layer, const void *k_new,
                        const void *v_new, int64_t suffix_tokens);
+
+// ---- pages of a pool -----------------------------------------------------------
+struct PagesArgs {
+    unsigned char *pool;
+    int64_t page_bytes;              // of one page of K (or of V): a multiple of 16
+    int32_t regions, num_pages;      // 2 * layers; pages of each
+    int32_t *counts;                 // device: tables that hold each page
+    int32_t *status;                 // device
+};
+hipError_t launch_pages_take(const PagesArgs &a, int32_t n, int32_t *out, int64_t stride, hipStream_t s);
+hipError_t launch_pages_copy(const PagesArgs &a, const int32_t *src, const int32_t *dst, int32_t n, hipStream_t s);
+// child c's table is children + c * stride; `full` whole pages are shared, and
+// with `part` one more is copied
+hipError_t launch_pages_fork(const PagesArgs &a, const int32_t *parent, int32_t full, bool part, int32_t n,
+                             int32_t *children, int64_t stride, hipStream_t s);
+hipError_t launch_pages_release(const PagesArgs &a, const int32_t *pages, int32_t n, hipStream_t s);
+// workspace: a move count, then the moves' sources, their targets and every page's new id
+size_t pages_workspace_bytes(int64_t num_pages);
+hipError_t launch_pages_compact(const PagesArgs &a, int32_t *tables, int32_t n_tables, int32_t entries,
+                                int64_t stride, int32_t *num_live, int32_t *ws, hipStream_t s);
 
 // ---- rest-of-layer compute window ---------------------------------------------
 struct LayerArgs {

@@ -1,0 +1,264 @@
+// Pages of a pool as they are shared, copied, freed and moved together.  The
+// state is one count per page, the number of tables that hold it; a page whose
+// count is not positive is free.  Everything happens on the device and in
+// stream order: no call waits for the host.
+//
+// Two kinds of kernel.  A plan (which pages are free, which move where) is one
+// workgroup's scan over the counts, 16 pages to a thread: 4 bytes a page.  The copies
+// are 16-byte pieces with remapped pages, bound by memory.
+#include <algorithm>
+
+#include "common.hpp"
+
+namespace oc {
+
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+
+constexpr int kCopyThreads = 256;
+constexpr int kSegment = kCopyThreads * 8 * 16;       // bytes of one workgroup's piece of a page
+constexpr int kPlanThreads = 1024, kPlanPages = 16;   // pages of a plan's thread and step
+
+// Copy `bytes` (a multiple of 16, at most kSegment) with one workgroup: eight
+// loads of a thread in flight.  Read once, written once: both sides past the caches.
+__device__ inline void copy_segment(const unsigned char *src, unsigned char *dst, int bytes) {
+    u32x4 x[8];
+    const int t = (int)threadIdx.x * 16;
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+        if (t + i * kCopyThreads * 16 < bytes)
+            x[i] = __builtin_nontemporal_load(reinterpret_cast<const u32x4 *>(src + t + i * kCopyThreads * 16));
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+        if (t + i * kCopyThreads * 16 < bytes)
+            __builtin_nontemporal_store(x[i], reinterpret_cast<u32x4 *>(dst + t + i * kCopyThreads * 16));
+}
+
+// Segment `item` of the copies of n pairs of pages: every region of a pair in
+// turn.  Pairs with an id outside the pool are left out.
+__device__ inline void copy_item(const PagesArgs &a, int64_t item, int32_t src, int32_t dst) {
+    const int segments = (int)((a.page_bytes + kSegment - 1) / kSegment);
+    const int64_t in_pair = item % ((int64_t)a.regions * segments);
+    const int region = (int)(in_pair / segments), seg = (int)(in_pair - (int64_t)region * segments);
+    if ((uint32_t)src >= (uint32_t)a.num_pages || (uint32_t)dst >= (uint32_t)a.num_pages) return;
+    unsigned char *const base = a.pool + (int64_t)region * a.num_pages * a.page_bytes + (int64_t)seg * kSegment;
+    const int64_t left = a.page_bytes - (int64_t)seg * kSegment;
+    copy_segment(base + src * a.page_bytes, base + dst * a.page_bytes, (int)(left < kSegment ? left : kSegment));
+}
+static int64_t copy_items(const PagesArgs &a, int64_t n) {
+    return n * a.regions * ((a.page_bytes + kSegment - 1) / kSegment);
+}
+__device__ inline int64_t items_per_pair(const PagesArgs &a) {
+    return (int64_t)a.regions * ((a.page_bytes + kSegment - 1) / kSegment);
+}
+
+__global__ __launch_bounds__(kCopyThreads) void pages_copy_kernel(PagesArgs a, const int32_t *src, const int32_t *dst,
+                                                                  int64_t items) {
+    const int64_t per = items_per_pair(a);
+    for (int64_t i = blockIdx.x; i < items; i += gridDim.x) copy_item(a, i, src[i / per], dst[i / per]);
+}
+
+// Exclusive sum of x over the workgroup's threads; the total in every thread.
+__device__ inline uint32_t block_scan(uint32_t x, uint32_t *total, uint32_t *lds) {
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    uint32_t s = x;
+#pragma unroll
+    for (int d = 1; d < 64; d <<= 1) {
+        const uint32_t y = __shfl_up(s, d);
+        if (lane >= d) s += y;
+    }
+    __syncthreads();                                  // the last call's sums have been read
+    if (lane == 63) lds[wave] = s;
+    __syncthreads();
+    uint32_t before = 0, all = 0;
+    for (int w = 0; w < kPlanThreads / 64; ++w) {
+        before += w < wave ? lds[w] : 0;
+        all += lds[w];
+    }
+    *total = all;
+    return before + s - x;
+}
+
+// Which of this thread's kPlanPages pages from `first` on are held (one bit each).
+__device__ inline uint32_t held_pages(const int32_t *counts, int64_t first, int32_t num_pages) {
+    typedef int32_t i32x4 __attribute__((ext_vector_type(4), aligned(4)));
+    uint32_t held = 0;
+    if (first + kPlanPages <= num_pages) {
+        i32x4 c[kPlanPages / 4];
+#pragma unroll
+        for (int i = 0; i < kPlanPages / 4; ++i) c[i] = *reinterpret_cast<const i32x4 *>(counts + first + i * 4);
+#pragma unroll
+        for (int i = 0; i < kPlanPages; ++i) held |= (uint32_t)(c[i / 4][i % 4] > 0) << i;
+        return held;
+    }
+#pragma unroll
+    for (int i = 0; i < kPlanPages; ++i)
+        if (first + i < num_pages) held |= (uint32_t)(counts[first + i] > 0) << i;
+    return held;
+}
+__device__ inline uint32_t pages_below(int64_t first, int64_t limit) {
+    const int64_t n = limit - first;
+    return n <= 0 ? 0u : n >= kPlanPages ? (1u << kPlanPages) - 1 : (1u << n) - 1;
+}
+
+// The n lowest free pages, in order, to out[i * stride], with a count of 1;
+// *status 0.  With fewer than n free: -1 to all of them, *status OC_ENOMEM, the
+// counts as they were.
+__global__ __launch_bounds__(kPlanThreads) void pages_take_kernel(PagesArgs a, int32_t n, int32_t *out, int64_t stride) {
+    __shared__ uint32_t sums[kPlanThreads / 64];
+    constexpr int64_t STEP = (int64_t)kPlanThreads * kPlanPages;
+    int64_t found = 0;
+    for (int64_t p0 = 0; p0 < a.num_pages && found < n; p0 += STEP) {
+        const int64_t first = p0 + (int64_t)threadIdx.x * kPlanPages;
+        uint32_t free = ~held_pages(a.counts, first, a.num_pages) & pages_below(first, a.num_pages), total;
+        int64_t at = found + block_scan((uint32_t)__popc(free), &total, sums);
+        for (; free && at < n; free &= free - 1, ++at) out[at * stride] = (int32_t)(first + __ffs(free) - 1);
+        found += total;
+    }
+    __syncthreads();
+    for (int64_t i = threadIdx.x; i < n; i += kPlanThreads) {
+        if (found >= n) a.counts[out[i * stride]] = 1;
+        else out[i * stride] = -1;
+    }
+    if (threadIdx.x == 0) *a.status = found >= n ? OC_OK : OC_ENOMEM;
+}
+
+// The children's tables and the counts of the shared pages, and the copies of
+// the parent's last, partial page (the children's own pages are in their tables).
+__global__ __launch_bounds__(kCopyThreads) void pages_fork_kernel(PagesArgs a, const int32_t *parent, int32_t full,
+                                                                  int32_t part, int32_t n, int32_t *children,
+                                                                  int64_t stride, int64_t items) {
+    if (part) {
+        if (*a.status != OC_OK) return;
+    } else if (blockIdx.x == 0 && threadIdx.x == 0) {
+        *a.status = OC_OK;
+    }
+    for (int64_t i = (int64_t)blockIdx.x * kCopyThreads + threadIdx.x; i < full; i += (int64_t)gridDim.x * kCopyThreads) {
+        const int32_t p = parent[i];
+        if ((uint32_t)p < (uint32_t)a.num_pages) atomicAdd(a.counts + p, n);
+        for (int c = 0; c < n; ++c) children[c * stride + i] = p;
+    }
+    const int64_t per = items_per_pair(a);
+    for (int64_t i = blockIdx.x; i < items; i += gridDim.x)
+        copy_item(a, i, parent[full], children[i / per * stride + full]);
+}
+
+__global__ __launch_bounds__(kCopyThreads) void pages_release_kernel(PagesArgs a, const int32_t *pages, int32_t n) {
+    const int64_t i = (int64_t)blockIdx.x * kCopyThreads + threadIdx.x;
+    if (i >= n) return;
+    const int32_t p = pages[i];
+    if ((uint32_t)p < (uint32_t)a.num_pages) atomicSub(a.counts + p, 1);
+}
+
+// Workspace of a compaction, in 32-bit words: [0] moves; from 16 on the
+// sources, the targets, and every page's new id.
+__device__ __host__ inline int64_t ws_src(int64_t) { return 16; }
+__device__ __host__ inline int64_t ws_dst(int64_t P) { return 16 + (P / 2 + 1); }
+__device__ __host__ inline int64_t ws_map(int64_t P) { return 16 + 2 * (P / 2 + 1); }
+
+// With `live` pages held, those at or behind `live` move, in order, to the free
+// ones before it, in order: as many of each, and no page is read and written.
+__global__ __launch_bounds__(kPlanThreads) void pages_plan_kernel(PagesArgs a, int32_t *ws, int32_t *num_live) {
+    __shared__ uint32_t sums[kPlanThreads / 64];
+    constexpr int64_t STEP = (int64_t)kPlanThreads * kPlanPages;
+    const int64_t P = a.num_pages;
+    int32_t *const src = ws + ws_src(P), *const dst = ws + ws_dst(P), *const map = ws + ws_map(P);
+    uint32_t total;
+    int64_t live = 0;
+    for (int64_t p0 = 0; p0 < P; p0 += STEP) {
+        (void)block_scan((uint32_t)__popc(held_pages(a.counts, p0 + (int64_t)threadIdx.x * kPlanPages, a.num_pages)), &total, sums);
+        live += total;
+    }
+    int64_t moves = 0, holes = 0;
+    for (int64_t p0 = 0; p0 < P; p0 += STEP) {
+        const int64_t first = p0 + (int64_t)threadIdx.x * kPlanPages;
+        const uint32_t held = held_pages(a.counts, first, a.num_pages), low = pages_below(first, live);
+        uint32_t move = held & ~low, hole = ~held & low;
+        // both counts in one sum: at most 2^14 each in a step
+        const uint32_t at = block_scan((uint32_t)__popc(move) | (uint32_t)__popc(hole) << 16, &total, sums);
+        int64_t m = moves + (at & 0xFFFFu), k = holes + (at >> 16);
+        // (the bounds hold unless another stream changes the counts meanwhile)
+        for (; move && m <= P / 2; move &= move - 1, ++m) src[m] = (int32_t)(first + __ffs(move) - 1);
+        for (; hole && k <= P / 2; hole &= hole - 1, ++k) dst[k] = (int32_t)(first + __ffs(hole) - 1);
+        for (int i = 0; i < kPlanPages && first + i < P; ++i) map[first + i] = (int32_t)(first + i);
+        moves += total & 0xFFFFu;
+        holes += total >> 16;
+    }
+    __syncthreads();
+    if (moves > holes) moves = holes;
+    if (moves > P / 2) moves = P / 2;
+    for (int64_t i = threadIdx.x; i < moves; i += kPlanThreads) {
+        const int32_t s = src[i], d = dst[i];
+        map[s] = d;
+        a.counts[d] = a.counts[s];
+        a.counts[s] = 0;
+    }
+    if (threadIdx.x == 0) {
+        ws[0] = (int32_t)moves;
+        *num_live = (int32_t)live;
+    }
+}
+
+__global__ __launch_bounds__(kCopyThreads) void pages_move_kernel(PagesArgs a, int32_t *tables, int32_t entries,
+                                                                  int64_t stride, int64_t n_entries, const int32_t *ws) {
+    const int32_t *const src = ws + ws_src(a.num_pages), *const dst = ws + ws_dst(a.num_pages), *const map = ws + ws_map(a.num_pages);
+    for (int64_t i = (int64_t)blockIdx.x * kCopyThreads + threadIdx.x; i < n_entries; i += (int64_t)gridDim.x * kCopyThreads) {
+        int32_t *const e = tables + i / entries * stride + i % entries;
+        const int32_t p = *e;
+        if ((uint32_t)p < (uint32_t)a.num_pages) *e = map[p];
+    }
+    const int64_t per = items_per_pair(a), items = (int64_t)ws[0] * per;
+    for (int64_t i = blockIdx.x; i < items; i += gridDim.x) copy_item(a, i, src[i / per], dst[i / per]);
+}
+
+// ---------------------------------------------------------------------------
+// host side
+// ---------------------------------------------------------------------------
+// workgroups of a copy: eight to a CU, each taking its next segment when one is done
+static unsigned copy_grid(int64_t items) { return (unsigned)std::max<int64_t>(1, std::min<int64_t>(items, 2048)); }
+
+hipError_t launch_pages_take(const PagesArgs &a, int32_t n, int32_t *out, int64_t stride, hipStream_t s) {
+    hipLaunchKernelGGL(pages_take_kernel, dim3(1), dim3(kPlanThreads), 0, s, a, n, out, stride);
+    return hipGetLastError();
+}
+
+hipError_t launch_pages_copy(const PagesArgs &a, const int32_t *src, const int32_t *dst, int32_t n, hipStream_t s) {
+    const int64_t items = copy_items(a, n);
+    hipLaunchKernelGGL(pages_copy_kernel, dim3(copy_grid(items)), dim3(kCopyThreads), 0, s, a, src, dst, items);
+    return hipGetLastError();
+}
+
+hipError_t launch_pages_fork(const PagesArgs &a, const int32_t *parent, int32_t full, bool part, int32_t n,
+                             int32_t *children, int64_t stride, hipStream_t s) {
+    if (part) {
+        const hipError_t e = launch_pages_take(a, n, children + full, stride, s);
+        if (e != hipSuccess) return e;
+    }
+    const int64_t items = part ? copy_items(a, n) : 0;
+    const unsigned grid = std::max(copy_grid(items), copy_grid(((int64_t)full + kCopyThreads - 1) / kCopyThreads));
+    hipLaunchKernelGGL(pages_fork_kernel, dim3(grid), dim3(kCopyThreads), 0, s, a, parent, full, (int32_t)part, n, children,
+                       stride, items);
+    return hipGetLastError();
+}
+
+hipError_t launch_pages_release(const PagesArgs &a, const int32_t *pages, int32_t n, hipStream_t s) {
+    hipLaunchKernelGGL(pages_release_kernel, dim3((unsigned)(((int64_t)n + kCopyThreads - 1) / kCopyThreads)),
+                       dim3(kCopyThreads), 0, s, a, pages, n);
+    return hipGetLastError();
+}
+
+size_t pages_workspace_bytes(int64_t num_pages) { return (size_t)(ws_map(num_pages) + num_pages) * 4; }
+
+hipError_t launch_pages_compact(const PagesArgs &a, int32_t *tables, int32_t n_tables, int32_t entries, int64_t stride,
+                                int32_t *num_live, int32_t *ws, hipStream_t s) {
+    hipLaunchKernelGGL(pages_plan_kernel, dim3(1), dim3(kPlanThreads), 0, s, a, ws, num_live);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+    // the moves are counted on the device: enough workgroups for as many as there can be
+    const int64_t n_entries = (int64_t)n_tables * entries;
+    const unsigned grid = std::max(copy_grid(copy_items(a, a.num_pages / 2)), copy_grid((n_entries + kCopyThreads - 1) / kCopyThreads));
+    hipLaunchKernelGGL(pages_move_kernel, dim3(grid), dim3(kCopyThreads), 0, s, a, tables, std::max(entries, 1), stride,
+                       n_entries, ws);
+    return hipGetLastError();
+}
+
+}  // namespace oc
