@@ -10,14 +10,12 @@
 #include <algorithm>
 
 #include "kv4.hpp"
-#include "mfma_tiles.hpp"
+#include "attention_tiles.hpp"
 
 namespace oc {
 
-constexpr int PAGE4 = 16;         // tokens per page
 constexpr int UNIT4 = 32;         // keys per unit: two pages
 constexpr int NW4 = 8;            // wavefronts of a workgroup
-constexpr float SLACK4 = 8.0f;    // log2 units the running maximum may lag
 
 struct Kv4Params {
     const uint16_t *q, *k_new, *v_new;
@@ -27,7 +25,7 @@ struct Kv4Params {
     float2 *ml_part;
     uint16_t *out;
     int64_t page_bytes, table_stride;
-    int code_bytes, Tp, Ts, rows, nq, nkv, grp, m_tiles, n_split, n_groups, units_per_split, max_tokens;
+    int code_bytes, Tp, Ts, rows, nq, nkv, grp, m_tiles, n_split, n_groups, n_units, units_per_split, max_tokens;
     float scale_log2;
 };
 
@@ -45,15 +43,14 @@ struct Kv4Params {
 // into LDS and read back transposed, four keys of one page per read.
 // ---------------------------------------------------------------------------
 
-// 16-byte column of V row r (key in its page), XORed so that a wavefront's
-// writes of one column step and its transposing reads each touch every bank once
-template <int D>
-__device__ __forceinline__ int v4_swz(int r) {
-    if constexpr (D == 128) return ((r & 7) << 1) | ((r >> 3) & 1);
-    else return (((r >> 1) & 3) << 1) | ((r >> 3) & 1);
-}
+// XOR on the 16-byte column of V row r (key in its page).  The columns of eight
+// rows that a write takes at once differ in their low three bits, and so do the 32-byte
+// pairs of the four rows that a transposing read takes at once, so neither meets on
+// a bank.  (An XOR by 2 * (r % 8) + r / 8 let every write meet another: 163 LDS cycles a
+// unit of one row tile, not 99.)
+__device__ __forceinline__ int v4_swz(int r) { return ((r & 3) << 1) | ((r >> 2) & 1); }
 
-// codes and scale byte of this lane's piece of one page
+// codes and scale byte of this lane's quarter of its key's row, K's or V's
 template <int D>
 struct Piece4 {
     uint32_t c[D / 32], b;
@@ -75,6 +72,9 @@ __device__ __forceinline__ Piece4<D> load_piece4(const unsigned char *page, uint
     return r;
 }
 
+// max(a, b) in one instruction, NaN left aside; fmaxf() quiets each operand with another
+__device__ __forceinline__ float max2(float a, float b) { return __builtin_amdgcn_fmed3f(a, b, __builtin_inff()); }
+
 // maximum (and sum) over the four lanes of a query row
 __device__ __forceinline__ float row_max(float x) {
     x = fmaxf(x, __shfl_xor(x, 16));
@@ -85,10 +85,10 @@ __device__ __forceinline__ float row_sum(float x) {
     return x + __shfl_xor(x, 32);
 }
 
-template <int D, int NR, bool DECODE>
-__global__ __launch_bounds__(NW4 * 64) void kv4_ways_kernel(Kv4Params p) {
+template <int D, int NR, int PF, bool DECODE>
+__global__ __launch_bounds__(NW4 * 64, NR == 1 ? 4 : 2) void kv4_ways_kernel(Kv4Params p) {
     constexpr int ROWS = 16 * NR, NDS = D / 32, NT = D / 16;
-    constexpr int TILE = PAGE4 * D;                       // V elements of one page
+    constexpr int TILE = PAGE * D;                       // V elements of one page
     constexpr int RING = 2 * TILE;                        // elements per wavefront; later 16 rows of O in fp32
     extern __shared__ __align__(1024) uint16_t lds[];     // [NW4][RING], then (m, l) [NW4][ROWS]
     const int tid = threadIdx.x, lane = tid & 63;
@@ -97,7 +97,8 @@ __global__ __launch_bounds__(NW4 * 64) void kv4_ways_kernel(Kv4Params p) {
 
     const int b = DECODE ? (int)blockIdx.y : 0;
     const int mt = (int)blockIdx.x / p.n_groups, gamma = (int)blockIdx.x - mt * p.n_groups;
-    const int h = gamma / p.n_split, split = gamma - h * p.n_split;
+    // decode: first splits, which every request has, next to each other, so that no XCD gets them all
+    const int h = DECODE ? gamma % p.nkv : gamma / p.n_split, split = DECODE ? gamma / p.nkv : gamma - h * p.n_split;
     int Tp = p.Tp;
     if (DECODE) {
         Tp = p.num_tokens[b];
@@ -105,29 +106,25 @@ __global__ __launch_bounds__(NW4 * 64) void kv4_ways_kernel(Kv4Params p) {
         if (Tp > p.max_tokens) Tp = p.max_tokens;
     }
     const int Ts = p.Ts, rows = p.rows, grp = p.grp, nq = p.nq, nkv = p.nkv;
-    const int n_pre_pages = (Tp + PAGE4 - 1) / PAGE4, n_pre = (n_pre_pages + 1) / 2;
+    const int n_pre_pages = (Tp + PAGE - 1) / PAGE, n_pre = (n_pre_pages + 1) / 2;
     const uint16_t *const q_in = p.q + (int64_t)b * nq * D;
     const uint16_t *const k_new = p.k_new + ((int64_t)b * nkv + h) * D, *const v_new = p.v_new + ((int64_t)b * nkv + h) * D;
-    const __attribute__((address_space(4))) int32_t *pages_c =
-        (const __attribute__((address_space(4))) int32_t *)(p.pages + b * p.table_stride);
+    const int32_t *const pages = p.pages + b * p.table_stride;
+    const int64_t page_bytes = p.page_bytes;
+    const float scale_log2 = p.scale_log2;
 
     // units of this split: the prefix's, then the suffix's up to the tile's last token
     int row_hi = (mt + 1) * ROWS - 1;
     if (row_hi > rows - 1) row_hi = rows - 1;
     const int n_units = n_pre + row_hi / grp / UNIT4 + 1;
-    int per = p.units_per_split;
-    if (DECODE) {
-        // every request over the same number of splits at most, each of a unit per wavefront at least
-        per = (n_units + p.n_split - 1) / p.n_split;
-        if (per < NW4) per = NW4;
-    }
+    const int per = p.units_per_split;
     const int u0 = split * per;
     int u1 = u0 + per;
     if (u1 > n_units) u1 = n_units;
     if (DECODE && u0 >= n_units) return;
     const int n_used = DECODE ? (n_units + per - 1) / per : p.n_split;
 
-    const uint32_t head_codes = (uint32_t)h * (PAGE4 * D / 2), head_scales = (uint32_t)p.code_bytes + (uint32_t)h * (PAGE4 * D / 32);
+    const uint32_t head_codes = (uint32_t)h * (PAGE * D / 2), head_scales = (uint32_t)p.code_bytes + (uint32_t)h * (PAGE * D / 32);
     if (DECODE && split == 0 && mt == 0 && wave == NW4 - 1) {
         // the token joins the cache: K by the wavefront's first half, V by its second.
         // No lane of the launch reads this slot.
@@ -136,8 +133,8 @@ __global__ __launch_bounds__(NW4 * 64) void kv4_ways_kernel(Kv4Params p) {
             const u32x4 x = *reinterpret_cast<const u32x4 *>((kv ? v_new : k_new) + i * 8);
             uint32_t sb;
             const uint32_t codes = kv4_encode8(x, &sb);
-            const int slot = Tp % PAGE4;
-            unsigned char *page = (kv ? p.pool_v : p.pool_k) + (int64_t)pages_c[Tp / PAGE4] * p.page_bytes;
+            const int slot = Tp % PAGE;
+            unsigned char *page = (kv ? p.pool_v : p.pool_k) + (int64_t)pages[Tp / PAGE] * page_bytes;
             *reinterpret_cast<uint32_t *>(page + head_codes + slot * (D / 2) + i * 4) = codes;
             if ((i & 3) == 0) page[head_scales + slot * (D / 32) + i / 4] = (unsigned char)sb;
         }
@@ -168,24 +165,21 @@ __global__ __launch_bounds__(NW4 * 64) void kv4_ways_kernel(Kv4Params p) {
     }
 
     uint16_t *const V = lds + wave * RING;
-    const int v_put = c * D, v_sw = v4_swz<D>(c);         // this lane's V row of a page
+    const int v_put = c * D, v_sw = v4_swz(c);         // this lane's V row of a page
     const int tr = 4 * g + ((lane >> 2) & 3), tq = lane & 3;
-    const int v_get = tr * D + (tq & 1) * 4, v_x = (tq >> 1) ^ v4_swz<D>(tr);
+    const int v_get = tr * D + (tq & 1) * 4, v_x = (tq >> 1) ^ v4_swz(tr);
 
     // softmax of one unit's scores s (two pages), then O^T += V^T P
     auto finish = [&](f32x4 (&s)[NR][2]) {
         bf16x8 pp[NR];
 #pragma unroll
         for (int r = 0; r < NR; ++r) {
-            float mx[2] = {-__builtin_inff(), -__builtin_inff()};
+            float mx[2];
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                mx[0] = fmaxf(mx[0], s[r][0][e]);
-                mx[1] = fmaxf(mx[1], s[r][1][e]);
-            }
-            const float mu = fmaxf(mx[0], mx[1]) * p.scale_log2;
-            // the running maximum is raised, and O rescaled, only when a score exceeds it by 2^SLACK4
-            if (__any(mu > m[r] + SLACK4)) {
+            for (int i = 0; i < 2; ++i) mx[i] = max2(max2(s[r][i][0], s[r][i][1]), max2(s[r][i][2], s[r][i][3]));
+            const float mu = max2(mx[0], mx[1]) * scale_log2;
+            // the running maximum is raised, and O rescaled, only when a score exceeds it by 2^RESCALE_SLACK
+            if (__any(mu > m[r] + RESCALE_SLACK)) {
                 const float mn = fmaxf(m[r], row_max(mu));
                 const float alpha = __builtin_amdgcn_exp2f(m[r] - (mn == -__builtin_inff() ? 0.f : mn));
                 m[r] = mn;
@@ -196,7 +190,7 @@ __global__ __launch_bounds__(NW4 * 64) void kv4_ways_kernel(Kv4Params p) {
             const float m_use = m[r] == -__builtin_inff() ? 0.f : m[r];
             f32x8 e;
 #pragma unroll
-            for (int i = 0; i < 8; ++i) e[i] = __builtin_amdgcn_exp2f(fmaf(s[r][i >> 2][i & 3], p.scale_log2, -m_use));
+            for (int i = 0; i < 8; ++i) e[i] = __builtin_amdgcn_exp2f(fmaf(s[r][i >> 2][i & 3], scale_log2, -m_use));
             // bfloat16 P for the matrix cores; the sum is over the rounded values that the product uses
             const bf16x8 bp = __builtin_convertvector(e, bf16x8);
             pp[r] = bp;
@@ -223,62 +217,88 @@ __global__ __launch_bounds__(NW4 * 64) void kv4_ways_kernel(Kv4Params p) {
 
     // ---- prefix units ----
     const int first = u0 + wave, end_pre = u1 < n_pre ? u1 : n_pre;
-    // A unit's pages and this lane's slots in them, held to the last token's: what
-    // lies behind it is never read, and its scores are masked.
-    auto fetch = [&](int u, Piece4<D> (&k)[2], Piece4<D> (&v)[2]) {
+    // The addresses of 64 pages at a time, one per lane, K's: a unit's come from there
+    // without a wait on memory.
+    uint64_t at = 0;
+    const int64_t kv_step = p.pool_v - p.pool_k;
+    auto load_ids = [&](int u) {
+        int pg = 2 * (u + (lane >> 1) * NW4) + (lane & 1);
+        if (pg > n_pre_pages - 1) pg = n_pre_pages - 1;
+        at = reinterpret_cast<uint64_t>(p.pool_k) + (uint64_t)((int64_t)pages[pg] * page_bytes);
+    };
+    auto code_at = [&](int slot) { return head_codes + slot * (D / 2) + g * (D / 8); };
+    auto scale_at = [&](int slot) { return head_scales + slot * (D / 32) + g * D / 128; };
+    const uint32_t my_code = code_at(c), my_scale = scale_at(c);
+    Piece4<D> k[PF][2], v[PF][2];
+    // the n-th unit of this wavefront, unit u of the prefix
+    auto fetch = [&](int n, int u, Piece4<D> (&k)[2], Piece4<D> (&v)[2]) {
+        if ((n & 31) == 0) load_ids(u);
+        uint32_t ca[2] = {my_code, my_code}, sa[2] = {my_scale, my_scale};
+        if ((u + 1) * UNIT4 > Tp) {
+            // slots behind the last token repeat it: they are masked, and never read
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                int pg = 2 * u + i;
+                if (pg > n_pre_pages - 1) pg = n_pre_pages - 1;
+                const int left = Tp - 1 - pg * PAGE, slot = c < left ? c : left;
+                ca[i] = code_at(slot);
+                sa[i] = scale_at(slot);
+            }
+        }
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
-            int pg = 2 * u + i;
-            if (pg > n_pre_pages - 1) pg = n_pre_pages - 1;
-            const int left = Tp - 1 - pg * PAGE4;
-            const uint32_t slot = (uint32_t)(c < left ? c : left);
-            const int64_t at = (int64_t)pages_c[pg] * p.page_bytes;
-            const uint32_t code_at = head_codes + slot * (D / 2) + g * (D / 8);
-            const uint32_t scale_at = head_scales + slot * (D / 32) + g * D / 128;
-            k[i] = load_piece4<D>(p.pool_k + at, code_at, scale_at);
-            v[i] = load_piece4<D>(p.pool_v + at, code_at, scale_at);
+            const int from = (2 * n + i) & 63;
+            const unsigned char *const base = reinterpret_cast<const unsigned char *>(
+                (uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)at, from) |
+                (uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)(at >> 32), from) << 32);
+            k[i] = load_piece4<D>(base, ca[i], sa[i]);
+            v[i] = load_piece4<D>(base + kv_step, ca[i], sa[i]);
         }
     };
-    Piece4<D> k[2], v[2];
-    if (first < end_pre) fetch(first, k, v);
-    for (int u = first; u < end_pre; u += NW4) {
-        Piece4<D> kc[2], vc[2];
-#pragma unroll
-        for (int i = 0; i < 2; ++i) {
-            kc[i] = k[i];
-            vc[i] = v[i];
-        }
-        if (u + NW4 < end_pre) fetch(u + NW4, k, v);
-#pragma unroll
-        for (int i = 0; i < 2; ++i) {
-            const float sc = kv4_scale(vc[i].b);
-#pragma unroll
-            for (int s = 0; s < NDS; ++s)
-                *reinterpret_cast<bf16x8 *>(V + i * TILE + v_put + (((g * NDS + s) ^ v_sw) << 3)) = kv4_decode8(vc[i].c[s], sc);
-        }
+    auto unit = [&](int n, int u, Piece4<D> (&k)[2], Piece4<D> (&v)[2]) {
         f32x4 s4[NR][2];
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
-            const float sc = kv4_scale(kc[i].b);
+            const float sc = kv4_scale(k[i].b);
 #pragma unroll
             for (int s = 0; s < NDS; ++s) {
-                const bf16x8 kf = kv4_decode8(kc[i].c[s], sc);
+                const bf16x8 kf = kv4_decode8(k[i].c[s], sc);
 #pragma unroll
                 for (int r = 0; r < NR; ++r)
                     s4[r][i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf, q[r][s], s == 0 ? f32x4{} : s4[r][i], 0, 0, 0);
             }
         }
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            const float sc = kv4_scale(v[i].b);
+#pragma unroll
+            for (int s = 0; s < NDS; ++s)
+                *reinterpret_cast<bf16x8 *>(V + i * TILE + v_put + (((g * NDS + s) ^ v_sw) << 3)) = kv4_decode8(v[i].c[s], sc);
+        }
+        // the codes are read: the unit PF further on takes their registers
+        if (u + PF * NW4 < end_pre) fetch(n, u + PF * NW4, k, v);
         if ((u + 1) * UNIT4 > Tp) {
 #pragma unroll
             for (int i = 0; i < 2; ++i)
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
-                    const bool seen = u * UNIT4 + i * PAGE4 + 4 * g + e < Tp;
+                    const bool seen = u * UNIT4 + i * PAGE + 4 * g + e < Tp;
 #pragma unroll
                     for (int r = 0; r < NR; ++r) s4[r][i][e] = seen ? s4[r][i][e] : -__builtin_inff();
                 }
         }
         finish(s4);
+    };
+#pragma unroll
+    for (int i = 0; i < PF; ++i)
+        if (first + i * NW4 < end_pre) fetch(i, first + i * NW4, k[i], v[i]);
+    for (int u = first, n = PF; u < end_pre; u += PF * NW4) {
+#pragma unroll
+        for (int i = 0; i < PF; ++i, ++n) {
+            const int ui = u + i * NW4;
+            if (ui >= end_pre) break;
+            unit(n, ui, k[i], v[i]);
+        }
     }
 
     // ---- suffix units ----
@@ -291,7 +311,7 @@ __global__ __launch_bounds__(NW4 * 64) void kv4_ways_kernel(Kv4Params p) {
         uint32_t odd = 0;                                 // a value of V is infinite or NaN
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
-            int T = t0 + i * PAGE4 + c;
+            int T = t0 + i * PAGE + c;
             if (T > Ts - 1) T = Ts - 1;                   // behind the last token: repeats it, masked
             const int64_t at = (int64_t)T * nkv * D + g * (D / 4);
             bf16x8 kf[NDS];
@@ -325,7 +345,7 @@ __global__ __launch_bounds__(NW4 * 64) void kv4_ways_kernel(Kv4Params p) {
                 for (int i = 0; i < 2; ++i)
 #pragma unroll
                     for (int e = 0; e < 4; ++e)
-                        s4[r][i][e] = t0 + i * PAGE4 + 4 * g + e <= tok[r] ? s4[r][i][e] : -__builtin_inff();
+                        s4[r][i][e] = t0 + i * PAGE + 4 * g + e <= tok[r] ? s4[r][i][e] : -__builtin_inff();
         }
         finish(s4);
         if (__any(odd != 0)) {
@@ -397,60 +417,397 @@ __global__ __launch_bounds__(NW4 * 64) void kv4_ways_kernel(Kv4Params p) {
     }
 }
 
+// ---------------------------------------------------------------------------
+// Many query rows: 256-row tiles, eight wavefronts of 32 rows each over the same
+// 64-key blocks, in the two-phase schedule of the bfloat16 kernel (a wavefront of
+// each SIMD in its matrix phase while the other does its softmax).
+//
+// Only the feed differs.  A wavefront owns one page of each block, waves 0-3 K's
+// and waves 4-7 V's: a prefix page's codes come into registers one block ahead (16
+// bytes and a scale byte per lane at d = 128), are decoded in a softmax phase, in the
+// shadow of the partner's MFMAs, and written to the swizzled bfloat16 tile; a suffix
+// page is copied straight to LDS.  Decoding costs 16 conversions per lane and block
+// beside some 130 vector operations of the softmax, and the codes a quarter of the
+// bytes, so the matrix phases bound this kernel as they do the bfloat16 one.
+// ---------------------------------------------------------------------------
+template <int D>
+__global__ __launch_bounds__(THREADS) void kv4_rows_kernel(Kv4Params p) {
+    constexpr int TILE = KB * D, NBUF = 4;
+    constexpr int NDW = D / 32;                    // dwords of codes per lane and page
+    constexpr int ND = PAGE * D * 2 / 1024;        // 1 KiB copies of a suffix page
+    constexpr int KROWS = 512 / D;                 // key rows per copy
+    extern __shared__ __align__(1024) uint16_t lds[];   // [NBUF][K tile, V tile], then a flag
+    __builtin_amdgcn_s_setprio(1);
+    const int tid = threadIdx.x, lane = tid & 63;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int col = lane & 31, half = lane >> 5;
+    const bool is_v = wave >= 4;
+    const int my_page = wave & 3;                  // of every block
+
+    const int m_tiles = p.m_tiles, n_split = p.n_split, grp = p.grp, nq = p.nq, nkv = p.nkv;
+    const int rows = p.rows, Tp = p.Tp, Ts = p.Ts, n_pre_pages = (Tp + PAGE - 1) / PAGE;
+    const float scale_log2 = p.scale_log2;
+    const int64_t page_bytes = p.page_bytes;
+    const unsigned char *const pool = is_v ? p.pool_v : p.pool_k;
+    const uint16_t *const dense = is_v ? p.v_new : p.k_new;
+    const __attribute__((address_space(4))) int32_t *pages_c =
+        (const __attribute__((address_space(4))) int32_t *)p.pages;
+    int gamma, mt;
+    if (!tile_of((int)blockIdx.x, m_tiles, p.n_groups, false, gamma, mt)) return;
+    const int g = gamma / n_split, split = gamma - g * n_split;
+
+    const int row = mt * TILE_ROWS + wave * WAVE_ROWS + col;
+    const bool row_ok = row < rows;
+    const int tok = row_ok ? row / grp : 0;
+    bf16x8 qop[D / 16];
+    {
+        const uint16_t *qr = p.q + ((int64_t)tok * nq + g * grp + (row_ok ? row % grp : 0)) * D + half * 8;
+#pragma unroll
+        for (int ds = 0; ds < D / 16; ++ds) qop[ds] = row_ok ? *reinterpret_cast<const bf16x8 *>(qr + ds * 16) : bf16x8{};
+    }
+
+    const int b0 = split * p.units_per_split;
+    int b1 = b0 + p.units_per_split, tok_max;
+    {   // causal clip: no row of this tile sees suffix keys past its last token
+        int row_hi = (mt + 1) * TILE_ROWS - 1;
+        if (row_hi > rows - 1) row_hi = rows - 1;
+        tok_max = row_hi / grp;
+        const int last = (n_pre_pages + tok_max / PAGE) / 4 + 1;
+        if (b1 > last) b1 = last;
+        if (b1 > p.n_units) b1 = p.n_units;
+    }
+    const int nb = b1 > b0 ? b1 - b0 : 0;
+    const int tok_tile = mt * TILE_ROWS / grp, tok_min = (mt * TILE_ROWS + wave * WAVE_ROWS) / grp;
+
+    // ---- this wavefront's page of a block ----
+    const int key = lane >> 2, piece = lane & 3;   // decoding: this lane's key row and quarter of it
+    const uint32_t code_at = (uint32_t)g * (PAGE * D / 2) + piece * (D / 8);
+    const uint32_t scale_at = (uint32_t)p.code_bytes + (uint32_t)g * (PAGE * D / 32) + piece * D / 128;
+    // V's swizzle moves whole 64-byte units, which all lanes would write in the same
+    // order and meet on a bank: a lane starts at a chunk of its own
+    const int rot = is_v ? (D == 128 ? key & 3 : (key >> 1) & 1) : 0;
+    auto page_of = [&](int j) { return (b0 + j) * 4 + my_page; };
+    auto load_pid = [&](int j) -> int {
+        int v = page_of(j);
+        if (v > n_pre_pages - 1) v = n_pre_pages - 1;
+        return v >= 0 ? pages_c[v] : 0;
+    };
+    struct Raw {
+        u32x4 c;
+        uint32_t b;
+    };
+    auto fetch = [&](int j, int pid) -> Raw {
+        Raw r{};
+        const int v = page_of(j);
+        if (v >= n_pre_pages) return r;
+        // slots behind the last token repeat it: they are masked, and never read
+        const int left = Tp - 1 - v * PAGE;
+        const uint32_t slot = (uint32_t)(key < left ? key : left);
+        const unsigned char *base = pool + (int64_t)pid * page_bytes;
+        if constexpr (D == 128) {
+            r.c = *reinterpret_cast<const u32x4 *>(base + code_at + slot * (D / 2));
+        } else {
+            const uint2 x = *reinterpret_cast<const uint2 *>(base + code_at + slot * (D / 2));
+            r.c = u32x4{x.x, x.y, 0, 0};
+        }
+        r.b = base[scale_at + slot * (D / 32)];
+        return r;
+    };
+    auto tile_k = [&](int j) -> uint16_t * { return lds + (j % NBUF) * 2 * TILE; };
+    auto tile_v = [&](int j) -> uint16_t * { return lds + (j % NBUF) * 2 * TILE + TILE; };
+    auto put = [&](int j, const Raw r) {
+        uint16_t *const page = (is_v ? tile_v(j) : tile_k(j)) + my_page * PAGE * D;
+        const int v = page_of(j);
+        if (v < n_pre_pages) {
+            const float sc = kv4_scale(r.b);
+            u32x4 c = r.c;
+            if constexpr (D == 128) {
+                c = rot & 1 ? __builtin_shufflevector(c, c, 1, 2, 3, 0) : c;
+                c = rot & 2 ? __builtin_shufflevector(c, c, 2, 3, 0, 1) : c;
+            } else {
+                c = rot ? __builtin_shufflevector(c, c, 1, 0, 2, 3) : c;
+            }
+            const int rr = my_page * PAGE + key;
+            const int swz = is_v ? v_swz<D>(key) : rr & (D / 8 - 1);
+#pragma unroll
+            for (int i = 0; i < NDW; ++i) {
+                const int chunk = piece * NDW + ((i + rot) & (NDW - 1));
+                *reinterpret_cast<bf16x8 *>(page + key * D + ((chunk ^ swz) << 3)) = kv4_decode8(c[i], sc);
+            }
+            return;
+        }
+#pragma unroll
+        for (int i = 0; i < ND; ++i) {
+            const int r0 = i * KROWS + lane / (D / 8);             // key row within the page
+            const int cc = (lane % (D / 8)) ^ (is_v ? v_swz<D>(r0) : r0 & (D / 8 - 1));
+            int T = (v - n_pre_pages) * PAGE + r0;
+            if (T > Ts - 1) T = Ts - 1;                            // rows past the last one repeat it (masked)
+            // below 2^31 bytes: the host limits T_s * n_kv * d * 2
+            dma16(dense, ((uint32_t)(T * nkv + g) * D + cc * 8) * 2, page + i * 512);
+        }
+    };
+    int pid = 0;
+    Raw raw{};
+    // into the buffer of block j - 2, whose last reads have ended (the schedule below)
+    auto refill = [&](int j) {
+        if (j + 2 < nb) put(j + 2, raw);
+        if (j + 3 < nb) {
+            raw = fetch(j + 3, pid);
+            pid = load_pid(j + 4);
+        }
+    };
+    // This wavefront's copies of block j have landed (its own writes are waited for by
+    // the barriers): behind a suffix page come only suffix pages.
+    auto await_block = [&](int j) {
+        if (page_of(j) < n_pre_pages) return;
+        if (j + 1 < nb) wait_vmcnt<ND>();
+        else wait_vmcnt<0>();
+    };
+
+    WaveState<D> w;
+#pragma unroll
+    for (int et = 0; et < D / 32; ++et) w.o[et] = f32x16{};
+    w.m = -__builtin_inff();
+    w.l = 0.f;
+    const int krow = key_perm(col);
+    int voff[D / 32];
+#pragma unroll
+    for (int et = 0; et < D / 32; ++et) voff[et] = vt_offset<D>(lane, et);
+
+    // Mask of one block, as in the bfloat16 kernel: keys below pe are prefix keys,
+    // suffix keys start at ps, and a row sees suffix key k when k - ps <= its token.
+    auto mask_block = [&](int b) {
+        const int sh = 8 * half;
+        const int pe = Tp - b * KB - sh, ps = n_pre_pages * PAGE - b * KB - sh, lim = tok + ps;
+#pragma unroll
+        for (int kt = 0; kt < 2; ++kt)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+                const int kin = kt * 32 + (i < 8 ? i : 8 + i);
+                const uint32_t keep = 0u - (uint32_t)((kin < pe) | ((kin >= ps) & (kin <= lim)));
+                w.s[kt][i] = __uint_as_float((__float_as_uint(w.s[kt][i]) & keep) | (0xff800000u & ~keep));
+            }
+    };
+    auto softmax_block = [&](int j) {
+        const int b = b0 + j;
+        if ((b + 1) * KB > Tp) {
+            const int ps = n_pre_pages * PAGE - b * KB, pe = Tp - b * KB;
+            const bool partial_prefix = ps > 0 && pe < (ps < KB ? ps : KB);
+            const bool unseen_suffix = ps < KB && KB - 1 - ps > tok_min;
+            if (partial_prefix || unseen_suffix) mask_block(b);
+        }
+        softmax_phase<D>(w, scale_log2);
+    };
+    // Wavefronts 4-7, in phase 2j, each on the V page that it has copied: where some
+    // row of the tile does not see a key of the page (its weight there is 0), only
+    // finite values may stand; what is taken out is added at the end, row by row.
+    uint32_t *const flag = reinterpret_cast<uint32_t *>(lds + NBUF * 2 * TILE);
+    auto finite_v = [&](int j) {
+        const int v = page_of(j);
+        if (j >= nb || v < n_pre_pages || (v - n_pre_pages) * PAGE + PAGE - 1 <= tok_tile) return;
+        uint16_t *const page = tile_v(j) + my_page * PAGE * D;
+        uint32_t odd = 0;
+#pragma unroll
+        for (int i = 0; i < ND; ++i) {
+            u32x4 x = *reinterpret_cast<const u32x4 *>(page + i * 512 + lane * 8);
+            uint32_t here = 0;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const uint32_t lo = (x[e] & 0x7F80u) == 0x7F80u ? 0xFFFFu : 0u;
+                const uint32_t hi = (x[e] & 0x7F800000u) == 0x7F800000u ? 0xFFFF0000u : 0u;
+                here |= lo | hi;
+                x[e] &= ~(lo | hi);
+            }
+            if (here) *reinterpret_cast<u32x4 *>(page + i * 512 + lane * 8) = x;
+            odd |= here;
+        }
+        if (odd) *flag = 1;
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+    };
+
+    if (tid == 0) *flag = 0;
+    __builtin_amdgcn_s_waitcnt(0x0F70);   // vmcnt(0): Q is in registers before the loop
+    if (nb > 0) {
+        const int p0 = load_pid(0), p1 = load_pid(1), p2 = load_pid(2);
+        pid = load_pid(3);
+        const Raw r0 = fetch(0, p0), r1 = nb > 1 ? fetch(1, p1) : Raw{};
+        if (nb > 2) raw = fetch(2, p2);
+        put(0, r0);
+        if (nb > 1) put(1, r1);
+    }
+    // The barriers and buffers are those of the bfloat16 kernel: block j + 2 is put in
+    // phase 2j by wavefronts 4-7 and in phase 2j + 1 by wavefronts 0-3, each of them at
+    // the start of a softmax phase; the barrier that ends their next matrix phase waits
+    // for their LDS writes, before phase 2j + 4, where the tile is first read.
+    auto softmax_end = [] { asm volatile("s_barrier" ::: "memory"); };
+    if (nb > 0) {
+        bf16x8 pre[LOOKAHEAD];
+        await_block(0);
+        lds_barrier();
+        if (!is_v) {
+            matrix_phase<D, false, true>(w, nullptr, voff, tile_k(0), qop, krow, half, pre);
+            lds_barrier();
+            refill(0);
+            softmax_block(0);
+            for (int j = 1; j < nb; ++j) {
+                prefetch_vt<D>(tile_v(j - 1), voff, pre);
+                await_block(j);
+                softmax_end();
+                matrix_phase<D, true, true>(w, tile_v(j - 1), voff, tile_k(j), qop, krow, half, pre);
+                lds_barrier();
+                refill(j);
+                softmax_block(j);
+            }
+            prefetch_vt<D>(tile_v(nb - 1), voff, pre);
+            softmax_end();
+            matrix_phase<D, true, false>(w, tile_v(nb - 1), voff, nullptr, qop, krow, half, pre);
+            lds_barrier();
+        } else {
+            refill(0);
+            finite_v(0);
+            lds_barrier();
+            matrix_phase<D, false, true>(w, nullptr, voff, tile_k(0), qop, krow, half, pre);
+            for (int j = 1; j < nb; ++j) {
+                await_block(j);
+                lds_barrier();
+                refill(j);
+                finite_v(j);
+                softmax_block(j - 1);
+                prefetch_vt<D>(tile_v(j - 1), voff, pre);
+                softmax_end();
+                matrix_phase<D, true, true>(w, tile_v(j - 1), voff, tile_k(j), qop, krow, half, pre);
+            }
+            lds_barrier();
+            softmax_block(nb - 1);
+            prefetch_vt<D>(tile_v(nb - 1), voff, pre);
+            softmax_end();
+            matrix_phase<D, true, false>(w, tile_v(nb - 1), voff, nullptr, qop, krow, half, pre);
+        }
+        if (*flag) {
+            // weights are positive, so a row carries the infinities and NaN of the keys it sees
+            int t0 = (b0 * 4 - n_pre_pages) * PAGE, t1 = (b1 * 4 - n_pre_pages) * PAGE;
+            if (t0 < 0) t0 = 0;
+            if (t1 > tok_max + 1) t1 = tok_max + 1;
+            for (int t = t0; t < t1; ++t) {
+                const uint16_t *vr = p.v_new + ((int64_t)t * nkv + g) * D;
+#pragma unroll
+                for (int et = 0; et < D / 32; ++et)
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) {
+                        const uint32_t x = (uint32_t)vr[et * 32 + (i >> 2) * 8 + half * 4 + (i & 3)] << 16;
+                        if ((x & 0x7F800000u) == 0x7F800000u && t <= tok) w.o[et][i] += __uint_as_float(x);
+                    }
+            }
+        }
+    }
+
+    const float l_tot = half_swap_sum(w.l);
+    if (!row_ok) return;
+    if (n_split == 1) {
+        const float inv = 1.f / l_tot;
+        uint16_t *orow = p.out + ((int64_t)tok * nq + g * grp + row % grp) * D;
+#pragma unroll
+        for (int et = 0; et < D / 32; ++et)
+#pragma unroll
+            for (int vq = 0; vq < 4; ++vq) {
+                f32x4 o4 = {w.o[et][vq * 4 + 0], w.o[et][vq * 4 + 1], w.o[et][vq * 4 + 2], w.o[et][vq * 4 + 3]};
+                *reinterpret_cast<bf16x4 *>(orow + et * 32 + vq * 8 + half * 4) = __builtin_convertvector(o4 * inv, bf16x4);
+            }
+    } else {
+        const int64_t prow = ((int64_t)split * nkv + g) * rows + row;
+        float *orow = p.o_part + prow * D;
+#pragma unroll
+        for (int et = 0; et < D / 32; ++et)
+#pragma unroll
+            for (int vq = 0; vq < 4; ++vq) {
+                f32x4 o4 = {w.o[et][vq * 4 + 0], w.o[et][vq * 4 + 1], w.o[et][vq * 4 + 2], w.o[et][vq * 4 + 3]};
+                *reinterpret_cast<f32x4 *>(orow + et * 32 + vq * 8 + half * 4) = o4;
+            }
+        if (half == 0) p.ml_part[prow] = float2{w.m, l_tot};
+    }
+}
+
 // Merge the splits of each row: weights 2^(m_s - M), normalised by the matching
-// sum of l_s.  d/4 threads per (KV head, row) of request blockIdx.y.
-template <int D, bool DECODE>
+// sum of l_s.  d/4 threads of four dimensions for a (KV head, row) of request
+// blockIdx.y, and SG such groups over the splits of one row: with many splits their
+// partials are all in flight at once (61 splits of four rows: 9.4 us with SG = 1).
+template <int D, bool DECODE, int SG>
 __global__ __launch_bounds__(256) void kv4_merge_kernel(Kv4Params p) {
-    constexpr int TPR = D / 4, RPB = 256 / TPR;
+    constexpr int TPR = D / 4, RPB = 256 / (TPR * SG), GS = 8;
     const int b = DECODE ? (int)blockIdx.y : 0;
-    const int64_t gr = (int64_t)blockIdx.x * RPB + threadIdx.x / TPR;
-    if (gr >= (int64_t)p.nkv * p.rows) return;
+    const int sg = (int)threadIdx.x / TPR % SG, c4 = (int)threadIdx.x % TPR, in = (int)threadIdx.x / (TPR * SG);
+    const int64_t gr = (int64_t)blockIdx.x * RPB + in;
     int n_split = p.n_split;
     if (DECODE) {
         int Tp = p.num_tokens[b];
         if (Tp < 0) return;
         if (Tp > p.max_tokens) Tp = p.max_tokens;
-        const int n_units = ((Tp + PAGE4 - 1) / PAGE4 + 1) / 2 + 1;
-        int per = (n_units + p.n_split - 1) / p.n_split;
-        if (per < NW4) per = NW4;
-        n_split = (n_units + per - 1) / per;
+        const int n_units = ((Tp + PAGE - 1) / PAGE + 1) / 2 + 1;
+        n_split = (n_units + p.units_per_split - 1) / p.units_per_split;
         if (n_split == 1) return;                         // written by the attention itself
     }
-    const int h = (int)(gr / p.rows), c4 = threadIdx.x % TPR;
-    const int64_t row = gr - (int64_t)h * p.rows, step = (int64_t)p.nkv * p.rows;
-    const int64_t prow0 = ((int64_t)b * p.n_split * p.nkv + h) * p.rows + row;
-    constexpr int GS = 8;
     float M = -__builtin_inff(), L = 0.f;
     f32x4 acc = {0.f, 0.f, 0.f, 0.f};
-    for (int s0 = 0; s0 < n_split; s0 += GS) {
-        float2 ml[GS];
-        f32x4 o[GS];
+    const bool ok = gr < (int64_t)p.nkv * p.rows;
+    const int h = ok ? (int)(gr / p.rows) : 0;
+    const int64_t row = ok ? gr - (int64_t)h * p.rows : 0;
+    if (ok) {
+        const int64_t step = (int64_t)p.nkv * p.rows;
+        const int64_t prow0 = ((int64_t)b * p.n_split * p.nkv + h) * p.rows + row;
+        for (int s0 = sg; s0 < n_split; s0 += SG * GS) {
+            float2 ml[GS];
+            f32x4 o[GS];
 #pragma unroll
-        for (int i = 0; i < GS; ++i) {
-            if (s0 + i < n_split) {
-                const int64_t prow = prow0 + (int64_t)(s0 + i) * step;
-                ml[i] = p.ml_part[prow];
-                o[i] = *reinterpret_cast<const f32x4 *>(p.o_part + prow * D + c4 * 4);
+            for (int i = 0; i < GS; ++i) {
+                if (s0 + i * SG < n_split) {
+                    const int64_t prow = prow0 + (int64_t)(s0 + i * SG) * step;
+                    ml[i] = p.ml_part[prow];
+                    o[i] = *reinterpret_cast<const f32x4 *>(p.o_part + prow * D + c4 * 4);
+                }
             }
-        }
-        float Mg = M;
+            float Mg = M;
 #pragma unroll
-        for (int i = 0; i < GS; ++i)
-            if (s0 + i < n_split) Mg = fmaxf(Mg, ml[i].x);
+            for (int i = 0; i < GS; ++i)
+                if (s0 + i * SG < n_split) Mg = fmaxf(Mg, ml[i].x);
+            const float Mu = Mg == -__builtin_inff() ? 0.f : Mg;
+            const float f = __builtin_amdgcn_exp2f(M - Mu);
+            L *= f;
+            acc *= f;
+#pragma unroll
+            for (int i = 0; i < GS; ++i) {
+                if (s0 + i * SG < n_split) {
+                    const float w = __builtin_amdgcn_exp2f(ml[i].x - Mu);
+                    L += w * ml[i].y;
+                    acc += w * o[i];
+                }
+            }
+            M = Mg;
+        }
+    }
+    if constexpr (SG > 1) {
+        __shared__ float part[RPB][SG][TPR][6];
+        float *const mine = part[in][sg][c4];
+        mine[0] = M;
+        mine[1] = L;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) mine[2 + i] = acc[i];
+        __syncthreads();
+        if (sg) return;
+        float Mg = M;
+        for (int x = 1; x < SG; ++x) Mg = fmaxf(Mg, part[in][x][c4][0]);
         const float Mu = Mg == -__builtin_inff() ? 0.f : Mg;
         const float f = __builtin_amdgcn_exp2f(M - Mu);
         L *= f;
         acc *= f;
+        for (int x = 1; x < SG; ++x) {
+            const float *const o = part[in][x][c4];
+            const float w = __builtin_amdgcn_exp2f(o[0] - Mu);
+            L += w * o[1];
 #pragma unroll
-        for (int i = 0; i < GS; ++i) {
-            if (s0 + i < n_split) {
-                const float w = __builtin_amdgcn_exp2f(ml[i].x - Mu);
-                L += w * ml[i].y;
-                acc += w * o[i];
-            }
+            for (int i = 0; i < 4; ++i) acc[i] += w * o[2 + i];
         }
-        M = Mg;
     }
+    if (!ok) return;
     uint16_t *orow = p.out + ((int64_t)b * p.nq + row / p.grp * p.nq + h * p.grp + row % p.grp) * D;
     *reinterpret_cast<bf16x4 *>(orow + c4 * 4) = __builtin_convertvector(acc * (1.f / L), bf16x4);
 }
@@ -464,8 +821,15 @@ static int attention_layout(const oc_layout &l) {
     const int rc = check_kv4_layout(l);
     if (rc) return rc;
     if (l.head_dim != 64 && l.head_dim != 128) return fail(OC_ESHAPE, "4-bit attention supports head_dim 64 or 128");
-    if (l.page_size != PAGE4) return fail(OC_ESHAPE, "4-bit attention supports page_size 16");
+    if (l.page_size != PAGE) return fail(OC_ESHAPE, "4-bit attention supports page_size 16");
     return OC_OK;
+}
+
+// workgroups of the 256-row kernel
+static int64_t rows_grid(const Kv4Plan &p) {
+    const int64_t groups = (int64_t)p.nkv * p.n_split;
+    if (groups <= INT32_MAX && tiles_by_xcd(p.m_tiles, (int)groups, false)) return (groups + 7) / 8 * 8 * p.m_tiles;
+    return groups * p.m_tiles;
 }
 
 static void size_workspace(Kv4Plan &p, int64_t requests) {
@@ -481,6 +845,9 @@ int plan_kv4_attention(const oc_layout &l, int64_t Tp, int64_t Ts, Kv4Plan *pl) 
     // key positions, query rows and their tokens are 32-bit in the kernels
     if (Tp > (int64_t)1 << 30 || Ts > (int64_t)1 << 30 || Tp + Ts > (int64_t)1 << 30)
         return fail(OC_ERANGE, "prefix + suffix tokens exceed 2^30");
+    // a tile's suffix rows are copied to LDS with 32-bit byte offsets from k_new / v_new
+    if (Ts * l.num_kv_heads > INT32_MAX / l.head_dim / 2)
+        return fail(OC_ERANGE, "suffix K/V of more than 2^31 bytes (suffix_tokens * n_kv * d * 2)");
     Kv4Plan p{};
     p.Tp = Tp;
     p.Ts = Ts;
@@ -490,16 +857,19 @@ int plan_kv4_attention(const oc_layout &l, int64_t Tp, int64_t Ts, Kv4Plan *pl) 
     p.d = l.head_dim;
     p.rows = Ts * p.grp;
     if (p.rows > (int64_t)1 << 30) return fail(OC_ERANGE, "suffix_tokens * (n_q / n_kv) exceeds 2^30");
-    p.row_tile = p.rows <= 16 ? 16 : 32;
+    p.row_tile = p.rows <= 16 ? 16 : p.rows <= 128 ? 32 : TILE_ROWS;
     p.m_tiles = (int)((p.rows + p.row_tile - 1) / p.row_tile);
-    p.n_units = (int)(((Tp + PAGE4 - 1) / PAGE4 + 1) / 2 + (Ts + UNIT4 - 1) / UNIT4);
+    const int64_t pre_pages = (Tp + PAGE - 1) / PAGE;
+    p.n_units = (int)(p.row_tile == TILE_ROWS ? (pre_pages + (Ts + PAGE - 1) / PAGE + 3) / 4
+                                              : (pre_pages + 1) / 2 + (Ts + UNIT4 - 1) / UNIT4);
     const int64_t tiles = (int64_t)p.nkv * p.m_tiles;
-    int64_t ns = std::max<int64_t>(1, std::min<int64_t>(512 / tiles, p.n_units / (2 * NW4)));
+    int64_t ns = std::max<int64_t>(1, p.row_tile == TILE_ROWS ? std::min<int64_t>(256 / tiles, p.n_units)
+                                                              : std::min<int64_t>(512 / tiles, p.n_units / (2 * NW4)));
     p.units_per_split = (int)((p.n_units + ns - 1) / ns);
     p.n_split = (p.n_units + p.units_per_split - 1) / p.units_per_split;
-    if (tiles * p.n_split > OC_MAX_GRID_ITEMS / (NW4 * 64))
+    if (rows_grid(p) > OC_MAX_GRID_ITEMS / (NW4 * 64))
         return fail(OC_ERANGE, "attention grid of more than 2^32 work-items");
-    if ((int64_t)p.nkv * p.rows * (p.d / 4) > OC_MAX_GRID_ITEMS)
+    if ((int64_t)p.nkv * p.rows * (p.d / 4) * 8 > OC_MAX_GRID_ITEMS)
         return fail(OC_ERANGE, "split merge grid exceeds 2^32 work-items");
     size_workspace(p, 1);
     *pl = p;
@@ -523,9 +893,10 @@ int plan_kv4_decode(const oc_layout &l, int64_t batch, int64_t max_tokens, Kv4Pl
     p.rows = p.grp;
     p.row_tile = p.rows <= 16 ? 16 : 32;
     p.m_tiles = (int)((p.rows + p.row_tile - 1) / p.row_tile);
-    p.n_units = (int)(((max_tokens + PAGE4 - 1) / PAGE4 + 1) / 2 + 1);
+    p.n_units = (int)(((max_tokens + PAGE - 1) / PAGE + 1) / 2 + 1);
     const int64_t tiles = batch * p.nkv * p.m_tiles;
-    const int64_t per = std::max<int64_t>(2 * NW4, (tiles * p.n_units + 2047) / 2048);
+    int64_t per = std::max<int64_t>(2 * NW4, (tiles * p.n_units + 2047) / 2048);
+    p.units_per_split = (int)per;
     p.n_split = (int)((p.n_units + per - 1) / per);
     if ((int64_t)p.nkv * p.m_tiles * p.n_split > OC_MAX_GRID_ITEMS / (NW4 * 64))
         return fail(OC_ERANGE, "attention grid of more than 2^32 work-items");
@@ -534,8 +905,8 @@ int plan_kv4_decode(const oc_layout &l, int64_t batch, int64_t max_tokens, Kv4Pl
     return OC_OK;
 }
 
-template <int D, int NR, bool DECODE>
-static hipError_t launch_ways4(const Kv4Plan &pl, const Kv4AttnArgs &a, hipStream_t s) {
+template <int D>
+static Kv4Params make_params(const Kv4Plan &pl, const Kv4AttnArgs &a) {
     Kv4Params p{};
     p.q = a.q;
     p.k_new = a.k_new;
@@ -559,30 +930,57 @@ static hipError_t launch_ways4(const Kv4Plan &pl, const Kv4AttnArgs &a, hipStrea
     p.m_tiles = pl.m_tiles;
     p.n_split = pl.n_split;
     p.n_groups = pl.nkv * pl.n_split;
+    p.n_units = pl.n_units;
     p.units_per_split = pl.units_per_split;
     p.max_tokens = a.max_tokens;
     p.scale_log2 = (float)(1.4426950408889634 / sqrt((double)D));
-    constexpr int LDS = NW4 * 2 * PAGE4 * D * 2 + NW4 * 16 * NR * 8;
-    static_assert(16 * D * 4 == 2 * PAGE4 * D * 2, "the wavefronts' O takes the place of their V");
-    const hipError_t e = allow_dynamic_lds<&kv4_ways_kernel<D, NR, DECODE>>(LDS);
+    return p;
+}
+
+template <int D, bool DECODE>
+static void launch_merge(const Kv4Params &p, unsigned requests, hipStream_t s) {
+    if (p.n_split < 2) return;
+    constexpr int RPB = 256 / (D / 4);
+    const int64_t n = (int64_t)p.nkv * p.rows;
+    if (p.n_split > 8)
+        hipLaunchKernelGGL((kv4_merge_kernel<D, DECODE, 8>), dim3((unsigned)((n * 8 + RPB - 1) / RPB), requests), dim3(256), 0, s, p);
+    else
+        hipLaunchKernelGGL((kv4_merge_kernel<D, DECODE, 1>), dim3((unsigned)((n + RPB - 1) / RPB), requests), dim3(256), 0, s, p);
+}
+
+template <int D>
+static hipError_t launch_rows(const Kv4Plan &pl, const Kv4AttnArgs &a, hipStream_t s) {
+    constexpr int LDS = 4 * 2 * KB * D * 2 + 16;
+    const hipError_t e = allow_dynamic_lds<&kv4_rows_kernel<D>>(LDS);
+    if (e != hipSuccess) return e;
+    const Kv4Params p = make_params<D>(pl, a);
+    hipLaunchKernelGGL(kv4_rows_kernel<D>, dim3((unsigned)rows_grid(pl)), dim3(THREADS), LDS, s, p);
+    launch_merge<D, false>(p, 1, s);
+    return hipGetLastError();
+}
+
+template <int D, int NR, int PF, bool DECODE>
+static hipError_t launch_ways4(const Kv4Plan &pl, const Kv4AttnArgs &a, hipStream_t s) {
+    const Kv4Params p = make_params<D>(pl, a);
+    constexpr int LDS = NW4 * 2 * PAGE * D * 2 + NW4 * 16 * NR * 8;
+    static_assert(16 * D * 4 == 2 * PAGE * D * 2, "the wavefronts' O takes the place of their V");
+    static_assert(NW4 * 64 == THREADS, "the grid's limit is shared");
+    const hipError_t e = allow_dynamic_lds<&kv4_ways_kernel<D, NR, PF, DECODE>>(LDS);
     if (e != hipSuccess) return e;
     const unsigned y = DECODE ? (unsigned)pl.batch : 1u;
-    hipLaunchKernelGGL((kv4_ways_kernel<D, NR, DECODE>), dim3((unsigned)(p.n_groups * pl.m_tiles), y), dim3(NW4 * 64), LDS, s, p);
-    if (p.n_split > 1) {
-        constexpr int RPB = 256 / (D / 4);
-        const int64_t blocks = ((int64_t)p.nkv * p.rows + RPB - 1) / RPB;
-        hipLaunchKernelGGL((kv4_merge_kernel<D, DECODE>), dim3((unsigned)blocks, y), dim3(256), 0, s, p);
-    }
+    hipLaunchKernelGGL((kv4_ways_kernel<D, NR, PF, DECODE>), dim3((unsigned)(p.n_groups * pl.m_tiles), y), dim3(NW4 * 64), LDS, s, p);
+    launch_merge<D, DECODE>(p, y, s);
     return hipGetLastError();
 }
 
 hipError_t launch_kv4_attention(const Kv4Plan &p, const Kv4AttnArgs &a, hipStream_t s) {
+    if (p.row_tile == TILE_ROWS) return p.d == 128 ? launch_rows<128>(p, a, s) : launch_rows<64>(p, a, s);
     if (p.batch) {
-        if (p.d == 128) return p.row_tile == 16 ? launch_ways4<128, 1, true>(p, a, s) : launch_ways4<128, 2, true>(p, a, s);
-        return p.row_tile == 16 ? launch_ways4<64, 1, true>(p, a, s) : launch_ways4<64, 2, true>(p, a, s);
+        if (p.d == 128) return p.row_tile == 16 ? launch_ways4<128, 1, 1, true>(p, a, s) : launch_ways4<128, 2, 2, true>(p, a, s);
+        return p.row_tile == 16 ? launch_ways4<64, 1, 2, true>(p, a, s) : launch_ways4<64, 2, 2, true>(p, a, s);
     }
-    if (p.d == 128) return p.row_tile == 16 ? launch_ways4<128, 1, false>(p, a, s) : launch_ways4<128, 2, false>(p, a, s);
-    return p.row_tile == 16 ? launch_ways4<64, 1, false>(p, a, s) : launch_ways4<64, 2, false>(p, a, s);
+    if (p.d == 128) return p.row_tile == 16 ? launch_ways4<128, 1, 1, false>(p, a, s) : launch_ways4<128, 2, 2, false>(p, a, s);
+    return p.row_tile == 16 ? launch_ways4<64, 1, 2, false>(p, a, s) : launch_ways4<64, 2, 2, false>(p, a, s);
 }
 
 }  // namespace oc
