@@ -25,7 +25,7 @@ struct Kv4Params {
     float2 *ml_part;
     uint16_t *out;
     int64_t page_bytes, table_stride;
-    int code_bytes, Tp, Ts, rows, nq, nkv, grp, m_tiles, n_split, n_groups, n_units, units_per_split, max_tokens;
+    int code_bytes, Tp, Ts, rows, nq, nkv, grp, m_tiles, n_split, n_groups, n_units, units_per_split, max_tokens, batch;
     float scale_log2;
 };
 
@@ -95,10 +95,23 @@ __global__ __launch_bounds__(NW4 * 64, NR == 1 ? 4 : 2) void kv4_ways_kernel(Kv4
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int c = lane & 15, g = lane >> 4;
 
-    const int b = DECODE ? (int)blockIdx.y : 0;
-    const int mt = (int)blockIdx.x / p.n_groups, gamma = (int)blockIdx.x - mt * p.n_groups;
-    // decode: first splits, which every request has, next to each other, so that no XCD gets them all
-    const int h = DECODE ? gamma % p.nkv : gamma / p.n_split, split = DECODE ? gamma / p.nkv : gamma - h * p.n_split;
+    int b = 0, h, mt, split;
+    if (DECODE) {
+        // first splits, which every request has, come first, and neighbours are of different
+        // heads and requests: no XCD gets the long ones
+        int i = (int)blockIdx.x;
+        const int pairs = p.batch * p.nkv;
+        split = i / pairs;
+        i -= split * pairs;
+        b = i / p.nkv;
+        h = i - b * p.nkv;
+        mt = (int)blockIdx.y;
+    } else {
+        mt = (int)blockIdx.x / p.n_groups;
+        const int gamma = (int)blockIdx.x - mt * p.n_groups;
+        h = gamma / p.n_split;
+        split = gamma - h * p.n_split;
+    }
     int Tp = p.Tp;
     if (DECODE) {
         Tp = p.num_tokens[b];
@@ -117,12 +130,15 @@ __global__ __launch_bounds__(NW4 * 64, NR == 1 ? 4 : 2) void kv4_ways_kernel(Kv4
     int row_hi = (mt + 1) * ROWS - 1;
     if (row_hi > rows - 1) row_hi = rows - 1;
     const int n_units = n_pre + row_hi / grp / UNIT4 + 1;
-    const int per = p.units_per_split;
-    const int u0 = split * per;
-    int u1 = u0 + per;
+    const int u0 = split * p.units_per_split;
+    int u1 = u0 + p.units_per_split, n_used = p.n_split;
+    if (DECODE) {
+        // the prefix's units are split, and the token's own goes with the last of them
+        n_used = n_pre > p.units_per_split ? (n_pre + p.units_per_split - 1) / p.units_per_split : 1;
+        if (split >= n_used) return;
+        if (split == n_used - 1) u1 = n_units;
+    }
     if (u1 > n_units) u1 = n_units;
-    if (DECODE && u0 >= n_units) return;
-    const int n_used = DECODE ? (n_units + per - 1) / per : p.n_split;
 
     const uint32_t head_codes = (uint32_t)h * (PAGE * D / 2), head_scales = (uint32_t)p.code_bytes + (uint32_t)h * (PAGE * D / 32);
     if (DECODE && split == 0 && mt == 0 && wave == NW4 - 1) {
@@ -742,8 +758,8 @@ __global__ __launch_bounds__(256) void kv4_merge_kernel(Kv4Params p) {
         int Tp = p.num_tokens[b];
         if (Tp < 0) return;
         if (Tp > p.max_tokens) Tp = p.max_tokens;
-        const int n_units = ((Tp + PAGE - 1) / PAGE + 1) / 2 + 1;
-        n_split = (n_units + p.units_per_split - 1) / p.units_per_split;
+        const int n_pre = ((Tp + PAGE - 1) / PAGE + 1) / 2;
+        n_split = n_pre > p.units_per_split ? (n_pre + p.units_per_split - 1) / p.units_per_split : 1;
         if (n_split == 1) return;                         // written by the attention itself
     }
     float M = -__builtin_inff(), L = 0.f;
@@ -832,10 +848,68 @@ static int64_t rows_grid(const Kv4Plan &p) {
     return groups * p.m_tiles;
 }
 
-static void size_workspace(Kv4Plan &p, int64_t requests) {
-    const int64_t rows = requests * p.n_split * p.nkv * p.rows;
+static void size_workspace(Kv4Plan &p) {
+    const int64_t rows = (int64_t)p.n_split * p.nkv * p.rows;
     p.off_ml = p.n_split > 1 ? up256((size_t)rows * p.d * 4) : 0;
     p.total = p.n_split > 1 ? p.off_ml + up256((size_t)rows * 8) : 256;
+}
+
+// Tiles and splits of one request's attention: `ns` key ranges at most.
+static Kv4Plan plan_tiles(const oc_layout &l, int64_t Tp, int64_t Ts, int row_tile, int64_t ns) {
+    Kv4Plan p{};
+    p.Tp = Tp;
+    p.Ts = Ts;
+    p.nq = l.num_q_heads;
+    p.nkv = l.num_kv_heads;
+    p.grp = p.nq / p.nkv;
+    p.d = l.head_dim;
+    p.rows = Ts * p.grp;
+    p.row_tile = row_tile;
+    p.m_tiles = (int)((p.rows + row_tile - 1) / row_tile);
+    const int64_t pre_pages = (Tp + PAGE - 1) / PAGE;
+    p.n_units = (int)(row_tile == TILE_ROWS ? (pre_pages + (Ts + PAGE - 1) / PAGE + 3) / 4
+                                            : (pre_pages + 1) / 2 + (Ts + UNIT4 - 1) / UNIT4);
+    ns = std::max<int64_t>(1, std::min<int64_t>(ns, p.n_units));
+    p.units_per_split = (int)((p.n_units + ns - 1) / ns);
+    p.n_split = (p.n_units + p.units_per_split - 1) / p.units_per_split;
+    size_workspace(p);
+    return p;
+}
+
+// Estimated time (us) of one request's attention under a plan: the rule that picks
+// the row tile and the splits.  Fitted to 75 shapes (n_q/n_kv/d of 32/8/128, 64/8/128,
+// 4/1/128, 6/2/128, 32/4/64, 8/8/64, 4/2/64; prefixes of 16 to 65536 tokens, suffixes
+// of 1 to 3584) with up to 30 plans each: over them the plan it picks is 2 % slower
+// than the best one measured, on average; it loses most (14 to 31 % on five shapes)
+// where several hundred new tokens follow a short prefix.
+struct Kv4Cost {
+    double unit128, unit64;     // one unit of one workgroup, at d = 128 and 64
+    double suffix;              // a suffix unit's extra (its rows are not fetched ahead)
+    double round;               // the least time of one unit per wavefront (row_tile 256: of a block)
+    double start;               // launch, first loads, epilogue
+    double wave;                // each further workgroup per CU
+};
+static const Kv4Cost COST4_16 = {0.132, 0.061, 0.197, 0.588, 4.9, 0.5}, COST4_32 = {0.184, 0.094, 0.191, 0.379, 6.1, 3.3},
+                     COST4_256 = {1.76, 1.32, 0., 1.32, 6.0, 0.};
+
+static double plan4_cost(const Kv4Plan &p) {
+    const bool large = p.row_tile == TILE_ROWS;
+    const Kv4Cost &k = p.row_tile == 16 ? COST4_16 : large ? COST4_256 : COST4_32;
+    const double pre = (double)((p.Tp + PAGE - 1) / PAGE), suf = (double)((p.Ts + PAGE - 1) / PAGE);
+    // average share of the keys that a row tile sees under the causal mask
+    const double seen = p.m_tiles > 1 ? (pre + 0.5 * (suf + 1)) / (pre + suf) : 1.0;
+    const double per_cu = (double)p.nkv * p.m_tiles * p.n_split / 256;
+    const double crowd = per_cu > 1 ? seen * std::max(1.0, std::min(std::ceil(per_cu), per_cu + 0.55)) : 1.0;
+    const double ups = p.units_per_split, suffix_units = std::min(ups, (double)((p.Ts + UNIT4 - 1) / UNIT4));
+    double body = ((p.d == 128 ? k.unit128 : k.unit64) * ups + k.suffix * suffix_units) * crowd;
+    body = std::max(body, k.round * (large ? ups : std::ceil(ups / NW4)));
+    // all inputs and the output once at 5 TB/s
+    const double hbm = p.d * (2.0 * p.nq * p.Ts + p.nkv * (1.0625 * p.Tp + 4.0 * p.Ts)) / 5e6;
+    double t = k.start + std::sqrt(body * body + hbm * hbm);
+    if (per_cu > 1) t += k.wave * (std::ceil(per_cu) - 1);
+    // the merge's launch, and its partials written and read
+    if (p.n_split > 1) t += 2.1 + 0.585e-6 * p.n_split * p.nkv * (double)p.rows * p.d * 4;
+    return t;
 }
 
 int plan_kv4_attention(const oc_layout &l, int64_t Tp, int64_t Ts, Kv4Plan *pl) {
@@ -845,37 +919,40 @@ int plan_kv4_attention(const oc_layout &l, int64_t Tp, int64_t Ts, Kv4Plan *pl) 
     // key positions, query rows and their tokens are 32-bit in the kernels
     if (Tp > (int64_t)1 << 30 || Ts > (int64_t)1 << 30 || Tp + Ts > (int64_t)1 << 30)
         return fail(OC_ERANGE, "prefix + suffix tokens exceed 2^30");
-    // a tile's suffix rows are copied to LDS with 32-bit byte offsets from k_new / v_new
+    // suffix rows are copied to LDS with 32-bit byte offsets from k_new / v_new
     if (Ts * l.num_kv_heads > INT32_MAX / l.head_dim / 2)
         return fail(OC_ERANGE, "suffix K/V of more than 2^31 bytes (suffix_tokens * n_kv * d * 2)");
-    Kv4Plan p{};
-    p.Tp = Tp;
-    p.Ts = Ts;
-    p.nq = l.num_q_heads;
-    p.nkv = l.num_kv_heads;
-    p.grp = p.nq / p.nkv;
-    p.d = l.head_dim;
-    p.rows = Ts * p.grp;
-    if (p.rows > (int64_t)1 << 30) return fail(OC_ERANGE, "suffix_tokens * (n_q / n_kv) exceeds 2^30");
-    p.row_tile = p.rows <= 16 ? 16 : p.rows <= 128 ? 32 : TILE_ROWS;
-    p.m_tiles = (int)((p.rows + p.row_tile - 1) / p.row_tile);
-    const int64_t pre_pages = (Tp + PAGE - 1) / PAGE;
-    p.n_units = (int)(p.row_tile == TILE_ROWS ? (pre_pages + (Ts + PAGE - 1) / PAGE + 3) / 4
-                                              : (pre_pages + 1) / 2 + (Ts + UNIT4 - 1) / UNIT4);
-    const int64_t tiles = (int64_t)p.nkv * p.m_tiles;
-    int64_t ns = std::max<int64_t>(1, p.row_tile == TILE_ROWS ? std::min<int64_t>(256 / tiles, p.n_units)
-                                                              : std::min<int64_t>(512 / tiles, p.n_units / (2 * NW4)));
-    p.units_per_split = (int)((p.n_units + ns - 1) / ns);
-    p.n_split = (p.n_units + p.units_per_split - 1) / p.units_per_split;
-    if (rows_grid(p) > OC_MAX_GRID_ITEMS / (NW4 * 64))
+    if (Ts * (l.num_q_heads / l.num_kv_heads) > (int64_t)1 << 30)
+        return fail(OC_ERANGE, "suffix_tokens * (n_q / n_kv) exceeds 2^30");
+    Kv4Plan best = plan_tiles(l, Tp, Ts, TILE_ROWS, 1);
+    double least = plan4_cost(best);
+    for (const int tile : {16, 32, TILE_ROWS})
+        for (const int ns : {1, 2, 3, 4, 6, 8, 12, 16, 24, 32, 48, 64}) {
+            const Kv4Plan p = plan_tiles(l, Tp, Ts, tile, ns);
+            const int64_t tiles = (int64_t)p.nkv * p.m_tiles;
+            if (tile != TILE_ROWS && tiles > 2048) continue;       // long suffixes: 256-row tiles
+            if (ns > 1 && (ns > p.n_units || tiles * ns > 1024)) break;
+            const double t = plan4_cost(p);
+            if (t < least) {
+                least = t;
+                best = p;
+            }
+        }
+    if (rows_grid(best) > OC_MAX_GRID_ITEMS / THREADS)
         return fail(OC_ERANGE, "attention grid of more than 2^32 work-items");
-    if ((int64_t)p.nkv * p.rows * (p.d / 4) * 8 > OC_MAX_GRID_ITEMS)
+    if ((int64_t)best.nkv * best.rows * (best.d / 4) * 8 > OC_MAX_GRID_ITEMS)
         return fail(OC_ERANGE, "split merge grid exceeds 2^32 work-items");
-    size_workspace(p, 1);
-    *pl = p;
+    *pl = best;
     return OC_OK;
 }
 
+// Decode: the prefix units of each (request, KV head) in ranges of one length for all
+// requests, as many as its length has.  If all were as long as they may be, every CU
+// would get a workgroup, and requests much longer than the others are cut into ranges
+// of at most 160 units (some 30 us).  Up to 24 units are one range: a merge costs
+// 2.5 us, as much as two or three units per wavefront.  Many more ranges cost as
+// well: a workgroup that finds its request shorter takes 2 ns of the whole card (32
+// requests of up to 28560 tokens: 61 us in ranges of 96, 86 in ranges of 16).
 int plan_kv4_decode(const oc_layout &l, int64_t batch, int64_t max_tokens, Kv4Plan *pl) {
     const int rc = attention_layout(l);
     if (rc) return rc;
@@ -893,14 +970,20 @@ int plan_kv4_decode(const oc_layout &l, int64_t batch, int64_t max_tokens, Kv4Pl
     p.rows = p.grp;
     p.row_tile = p.rows <= 16 ? 16 : 32;
     p.m_tiles = (int)((p.rows + p.row_tile - 1) / p.row_tile);
-    p.n_units = (int)(((max_tokens + PAGE - 1) / PAGE + 1) / 2 + 1);
-    const int64_t tiles = batch * p.nkv * p.m_tiles;
-    int64_t per = std::max<int64_t>(2 * NW4, (tiles * p.n_units + 2047) / 2048);
-    p.units_per_split = (int)per;
-    p.n_split = (int)((p.n_units + per - 1) / per);
-    if ((int64_t)p.nkv * p.m_tiles * p.n_split > OC_MAX_GRID_ITEMS / (NW4 * 64))
-        return fail(OC_ERANGE, "attention grid of more than 2^32 work-items");
-    size_workspace(p, batch);
+    p.n_units = (int)(((max_tokens + PAGE - 1) / PAGE + 1) / 2);
+    const int64_t pairs = batch * p.nkv;
+    if (pairs > OC_MAX_GRID_ITEMS / THREADS) return fail(OC_ERANGE, "attention grid of more than 2^32 work-items");
+    const int64_t fill = std::max<int64_t>(1, 256 / (pairs * p.m_tiles));
+    int64_t ns = 1;
+    if (p.n_units > 3 * NW4) ns = (std::max<int64_t>(fill, (p.n_units + 159) / 160) + fill - 1) / fill * fill;
+    ns = std::min(ns, std::max<int64_t>(1, OC_MAX_GRID_ITEMS / THREADS / pairs));
+    const int64_t per = std::max<int64_t>(1, (p.n_units + ns - 1) / ns);
+    p.units_per_split = (int)((per + NW4 - 1) / NW4 * NW4);
+    p.n_split = std::max(1, (p.n_units + p.units_per_split - 1) / p.units_per_split);
+    if (pairs * p.rows * (p.d / 4) * 8 > OC_MAX_GRID_ITEMS) return fail(OC_ERANGE, "merge grid exceeds 2^32 work-items");
+    const int64_t rows = batch * p.n_split * p.nkv * p.rows;
+    p.off_ml = p.n_split > 1 ? up256((size_t)rows * p.d * 4) : 0;
+    p.total = p.n_split > 1 ? p.off_ml + up256((size_t)rows * 8) : 256;
     *pl = p;
     return OC_OK;
 }
@@ -933,6 +1016,7 @@ static Kv4Params make_params(const Kv4Plan &pl, const Kv4AttnArgs &a) {
     p.n_units = pl.n_units;
     p.units_per_split = pl.units_per_split;
     p.max_tokens = a.max_tokens;
+    p.batch = pl.batch;
     p.scale_log2 = (float)(1.4426950408889634 / sqrt((double)D));
     return p;
 }
@@ -967,9 +1051,9 @@ static hipError_t launch_ways4(const Kv4Plan &pl, const Kv4AttnArgs &a, hipStrea
     static_assert(NW4 * 64 == THREADS, "the grid's limit is shared");
     const hipError_t e = allow_dynamic_lds<&kv4_ways_kernel<D, NR, PF, DECODE>>(LDS);
     if (e != hipSuccess) return e;
-    const unsigned y = DECODE ? (unsigned)pl.batch : 1u;
-    hipLaunchKernelGGL((kv4_ways_kernel<D, NR, PF, DECODE>), dim3((unsigned)(p.n_groups * pl.m_tiles), y), dim3(NW4 * 64), LDS, s, p);
-    launch_merge<D, DECODE>(p, y, s);
+    const dim3 grid = DECODE ? dim3((unsigned)(p.n_groups * pl.batch), (unsigned)pl.m_tiles) : dim3((unsigned)(p.n_groups * pl.m_tiles));
+    hipLaunchKernelGGL((kv4_ways_kernel<D, NR, PF, DECODE>), grid, dim3(NW4 * 64), LDS, s, p);
+    launch_merge<D, DECODE>(p, DECODE ? (unsigned)pl.batch : 1u, s);
     return hipGetLastError();
 }
 
