@@ -19,14 +19,18 @@ constexpr int kSegment = kCopyThreads * 8 * 16;       // bytes of one workgroup'
 constexpr int kPlanThreads = 1024, kPlanPages = 16;   // pages of a plan's thread and step
 
 // Copy `bytes` (a multiple of 16, at most kSegment) with one workgroup: eight
-// loads of a thread in flight.  Read once, written once: both sides past the caches.
+// loads of a thread in flight.  What is written is not read again soon, so it
+// bypasses the caches; and so does what is read, unless several copies read it.
+template <bool REREAD>
 __device__ inline void copy_segment(const unsigned char *src, unsigned char *dst, int bytes) {
     u32x4 x[8];
     const int t = (int)threadIdx.x * 16;
 #pragma unroll
     for (int i = 0; i < 8; ++i)
-        if (t + i * kCopyThreads * 16 < bytes)
-            x[i] = __builtin_nontemporal_load(reinterpret_cast<const u32x4 *>(src + t + i * kCopyThreads * 16));
+        if (t + i * kCopyThreads * 16 < bytes) {
+            const u32x4 *from = reinterpret_cast<const u32x4 *>(src + t + i * kCopyThreads * 16);
+            x[i] = REREAD ? *from : __builtin_nontemporal_load(from);
+        }
 #pragma unroll
     for (int i = 0; i < 8; ++i)
         if (t + i * kCopyThreads * 16 < bytes)
@@ -35,6 +39,7 @@ __device__ inline void copy_segment(const unsigned char *src, unsigned char *dst
 
 // Segment `item` of the copies of n pairs of pages: every region of a pair in
 // turn.  Pairs with an id outside the pool are left out.
+template <bool REREAD>
 __device__ inline void copy_item(const PagesArgs &a, int64_t item, int32_t src, int32_t dst) {
     const int segments = (int)((a.page_bytes + kSegment - 1) / kSegment);
     const int64_t in_pair = item % ((int64_t)a.regions * segments);
@@ -42,7 +47,7 @@ __device__ inline void copy_item(const PagesArgs &a, int64_t item, int32_t src, 
     if ((uint32_t)src >= (uint32_t)a.num_pages || (uint32_t)dst >= (uint32_t)a.num_pages) return;
     unsigned char *const base = a.pool + (int64_t)region * a.num_pages * a.page_bytes + (int64_t)seg * kSegment;
     const int64_t left = a.page_bytes - (int64_t)seg * kSegment;
-    copy_segment(base + src * a.page_bytes, base + dst * a.page_bytes, (int)(left < kSegment ? left : kSegment));
+    copy_segment<REREAD>(base + src * a.page_bytes, base + dst * a.page_bytes, (int)(left < kSegment ? left : kSegment));
 }
 static int64_t copy_items(const PagesArgs &a, int64_t n) {
     return n * a.regions * ((a.page_bytes + kSegment - 1) / kSegment);
@@ -54,7 +59,7 @@ __device__ inline int64_t items_per_pair(const PagesArgs &a) {
 __global__ __launch_bounds__(kCopyThreads) void pages_copy_kernel(PagesArgs a, const int32_t *src, const int32_t *dst,
                                                                   int64_t items) {
     const int64_t per = items_per_pair(a);
-    for (int64_t i = blockIdx.x; i < items; i += gridDim.x) copy_item(a, i, src[i / per], dst[i / per]);
+    for (int64_t i = blockIdx.x; i < items; i += gridDim.x) copy_item<false>(a, i, src[i / per], dst[i / per]);
 }
 
 // Exclusive sum of x over the workgroup's threads; the total in every thread.
@@ -122,24 +127,31 @@ __global__ __launch_bounds__(kPlanThreads) void pages_take_kernel(PagesArgs a, i
     if (threadIdx.x == 0) *a.status = found >= n ? OC_OK : OC_ENOMEM;
 }
 
-// The children's tables and the counts of the shared pages, and the copies of
-// the parent's last, partial page (the children's own pages are in their tables).
+// The first `table_wgs` workgroups write the children's tables and the counts of the
+// shared pages; the others copy the parent's last, partial page to the children's
+// own, which are in their tables already (-1, and so no copy, where they did not get
+// one).
 __global__ __launch_bounds__(kCopyThreads) void pages_fork_kernel(PagesArgs a, const int32_t *parent, int32_t full,
                                                                   int32_t part, int32_t n, int32_t *children,
-                                                                  int64_t stride, int64_t items) {
-    if (part) {
-        if (*a.status != OC_OK) return;
-    } else if (blockIdx.x == 0 && threadIdx.x == 0) {
-        *a.status = OC_OK;
+                                                                  int64_t stride, int64_t items, int32_t table_wgs) {
+    if ((int)blockIdx.x >= table_wgs) {
+        const int64_t per = items_per_pair(a), wgs = (int64_t)gridDim.x - table_wgs;
+        for (int64_t i = (int64_t)blockIdx.x - table_wgs; i < items; i += wgs)
+            copy_item<true>(a, i, parent[full], children[i / per * stride + full]);
+        return;
     }
-    for (int64_t i = (int64_t)blockIdx.x * kCopyThreads + threadIdx.x; i < full; i += (int64_t)gridDim.x * kCopyThreads) {
-        const int32_t p = parent[i];
-        if ((uint32_t)p < (uint32_t)a.num_pages) atomicAdd(a.counts + p, n);
-        for (int c = 0; c < n; ++c) children[c * stride + i] = p;
+    if (!part) {
+        if (blockIdx.x == 0 && threadIdx.x == 0) *a.status = OC_OK;
+    } else if (*a.status != OC_OK) {
+        return;
     }
-    const int64_t per = items_per_pair(a);
-    for (int64_t i = blockIdx.x; i < items; i += gridDim.x)
-        copy_item(a, i, parent[full], children[i / per * stride + full]);
+    const int64_t entries = (int64_t)n * full;
+    for (int64_t i = (int64_t)blockIdx.x * kCopyThreads + threadIdx.x; i < entries; i += (int64_t)table_wgs * kCopyThreads) {
+        const int64_t c = i / full, e = i - c * full;
+        const int32_t p = parent[e];
+        children[c * stride + e] = p;
+        if (c == 0 && (uint32_t)p < (uint32_t)a.num_pages) atomicAdd(a.counts + p, n);
+    }
 }
 
 __global__ __launch_bounds__(kCopyThreads) void pages_release_kernel(PagesArgs a, const int32_t *pages, int32_t n) {
@@ -156,38 +168,63 @@ __device__ __host__ inline int64_t ws_dst(int64_t P) { return 16 + (P / 2 + 1); 
 __device__ __host__ inline int64_t ws_map(int64_t P) { return 16 + 2 * (P / 2 + 1); }
 
 // With `live` pages held, those at or behind `live` move, in order, to the free
-// ones before it, in order: as many of each, and no page is read and written.
+// ones before it, in order: as many of each, and no page is read and written.  With
+// b(p) held pages before page p, a free page p in front is the (p - b(p))-th target
+// and a held one behind the (b(p) - b(live))-th source, so one scan gives both.
 __global__ __launch_bounds__(kPlanThreads) void pages_plan_kernel(PagesArgs a, int32_t *ws, int32_t *num_live) {
+    constexpr int NEAR = 2048;                        // moves whose ids stay in LDS too
     __shared__ uint32_t sums[kPlanThreads / 64];
+    __shared__ int32_t near_src[NEAR], near_dst[NEAR];
+    __shared__ int64_t before_live;
     constexpr int64_t STEP = (int64_t)kPlanThreads * kPlanPages;
     const int64_t P = a.num_pages;
     int32_t *const src = ws + ws_src(P), *const dst = ws + ws_dst(P), *const map = ws + ws_map(P);
-    uint32_t total;
+    uint32_t held = 0, below = 0, total = 0;          // this thread's pages, those held before them, and in the step
     int64_t live = 0;
     for (int64_t p0 = 0; p0 < P; p0 += STEP) {
-        (void)block_scan((uint32_t)__popc(held_pages(a.counts, p0 + (int64_t)threadIdx.x * kPlanPages, a.num_pages)), &total, sums);
+        held = held_pages(a.counts, p0 + (int64_t)threadIdx.x * kPlanPages, a.num_pages);
+        below = block_scan((uint32_t)__popc(held), &total, sums);
         live += total;
     }
-    int64_t moves = 0, holes = 0;
+    int64_t run = 0;
     for (int64_t p0 = 0; p0 < P; p0 += STEP) {
         const int64_t first = p0 + (int64_t)threadIdx.x * kPlanPages;
-        const uint32_t held = held_pages(a.counts, first, a.num_pages), low = pages_below(first, live);
-        uint32_t move = held & ~low, hole = ~held & low;
-        // both counts in one sum: at most 2^14 each in a step
-        const uint32_t at = block_scan((uint32_t)__popc(move) | (uint32_t)__popc(hole) << 16, &total, sums);
-        int64_t m = moves + (at & 0xFFFFu), k = holes + (at >> 16);
+        if (P > STEP) {                               // else the pass above has them
+            held = held_pages(a.counts, first, a.num_pages);
+            below = block_scan((uint32_t)__popc(held), &total, sums);
+        }
+        const int64_t b = run + below;
+        if (live >= p0 && live < p0 + STEP) {         // the step that has page `live`: no source came before it
+            if (live >= first && live < first + kPlanPages)
+                before_live = b + __popc(held & ((1u << (live - first)) - 1));
+            __syncthreads();
+        }
+        const uint32_t low = pages_below(first, live), here = pages_below(first, P);
         // (the bounds hold unless another stream changes the counts meanwhile)
-        for (; move && m <= P / 2; move &= move - 1, ++m) src[m] = (int32_t)(first + __ffs(move) - 1);
-        for (; hole && k <= P / 2; hole &= hole - 1, ++k) dst[k] = (int32_t)(first + __ffs(hole) - 1);
+        for (uint32_t f = ~held & low; f; f &= f - 1) {
+            const int i = __ffs(f) - 1;
+            const int64_t k = first + i - b - __popc(held & ((1u << i) - 1));
+            if (k < 0 || k > P / 2) break;
+            dst[k] = (int32_t)(first + i);
+            if (k < NEAR) near_dst[k] = (int32_t)(first + i);
+        }
+        if (p0 + STEP > live) {
+            for (uint32_t f = held & here & ~low; f; f &= f - 1) {
+                const int i = __ffs(f) - 1;
+                const int64_t m = b + __popc(held & ((1u << i) - 1)) - before_live;
+                if (m < 0 || m > P / 2) break;
+                src[m] = (int32_t)(first + i);
+                if (m < NEAR) near_src[m] = (int32_t)(first + i);
+            }
+        }
         for (int i = 0; i < kPlanPages && first + i < P; ++i) map[first + i] = (int32_t)(first + i);
-        moves += total & 0xFFFFu;
-        holes += total >> 16;
+        run += total;
     }
     __syncthreads();
-    if (moves > holes) moves = holes;
+    int64_t moves = live < P ? live - before_live : 0;
     if (moves > P / 2) moves = P / 2;
     for (int64_t i = threadIdx.x; i < moves; i += kPlanThreads) {
-        const int32_t s = src[i], d = dst[i];
+        const int32_t s = i < NEAR ? near_src[i] : src[i], d = i < NEAR ? near_dst[i] : dst[i];
         map[s] = d;
         a.counts[d] = a.counts[s];
         a.counts[s] = 0;
@@ -198,16 +235,21 @@ __global__ __launch_bounds__(kPlanThreads) void pages_plan_kernel(PagesArgs a, i
     }
 }
 
+// The first `table_wgs` workgroups rewrite the tables, the others copy the pages.
 __global__ __launch_bounds__(kCopyThreads) void pages_move_kernel(PagesArgs a, int32_t *tables, int32_t entries,
-                                                                  int64_t stride, int64_t n_entries, const int32_t *ws) {
+                                                                  int64_t stride, int64_t n_entries, const int32_t *ws,
+                                                                  int32_t table_wgs) {
     const int32_t *const src = ws + ws_src(a.num_pages), *const dst = ws + ws_dst(a.num_pages), *const map = ws + ws_map(a.num_pages);
-    for (int64_t i = (int64_t)blockIdx.x * kCopyThreads + threadIdx.x; i < n_entries; i += (int64_t)gridDim.x * kCopyThreads) {
+    if ((int)blockIdx.x >= table_wgs) {
+        const int64_t per = items_per_pair(a), items = (int64_t)ws[0] * per, wgs = (int64_t)gridDim.x - table_wgs;
+        for (int64_t i = (int64_t)blockIdx.x - table_wgs; i < items; i += wgs) copy_item<false>(a, i, src[i / per], dst[i / per]);
+        return;
+    }
+    for (int64_t i = (int64_t)blockIdx.x * kCopyThreads + threadIdx.x; i < n_entries; i += (int64_t)table_wgs * kCopyThreads) {
         int32_t *const e = tables + i / entries * stride + i % entries;
         const int32_t p = *e;
         if ((uint32_t)p < (uint32_t)a.num_pages) *e = map[p];
     }
-    const int64_t per = items_per_pair(a), items = (int64_t)ws[0] * per;
-    for (int64_t i = blockIdx.x; i < items; i += gridDim.x) copy_item(a, i, src[i / per], dst[i / per]);
 }
 
 // ---------------------------------------------------------------------------
@@ -234,9 +276,9 @@ hipError_t launch_pages_fork(const PagesArgs &a, const int32_t *parent, int32_t 
         if (e != hipSuccess) return e;
     }
     const int64_t items = part ? copy_items(a, n) : 0;
-    const unsigned grid = std::max(copy_grid(items), copy_grid(((int64_t)full + kCopyThreads - 1) / kCopyThreads));
-    hipLaunchKernelGGL(pages_fork_kernel, dim3(grid), dim3(kCopyThreads), 0, s, a, parent, full, (int32_t)part, n, children,
-                       stride, items);
+    const unsigned tables = copy_grid(((int64_t)n * full + kCopyThreads - 1) / kCopyThreads);
+    hipLaunchKernelGGL(pages_fork_kernel, dim3(tables + copy_grid(items)), dim3(kCopyThreads), 0, s, a, parent, full, (int32_t)part,
+                       n, children, stride, items, (int32_t)tables);
     return hipGetLastError();
 }
 
@@ -255,9 +297,9 @@ hipError_t launch_pages_compact(const PagesArgs &a, int32_t *tables, int32_t n_t
     if (e != hipSuccess) return e;
     // the moves are counted on the device: enough workgroups for as many as there can be
     const int64_t n_entries = (int64_t)n_tables * entries;
-    const unsigned grid = std::max(copy_grid(copy_items(a, a.num_pages / 2)), copy_grid((n_entries + kCopyThreads - 1) / kCopyThreads));
-    hipLaunchKernelGGL(pages_move_kernel, dim3(grid), dim3(kCopyThreads), 0, s, a, tables, std::max(entries, 1), stride,
-                       n_entries, ws);
+    const unsigned table_wgs = copy_grid((n_entries + kCopyThreads - 1) / kCopyThreads);
+    hipLaunchKernelGGL(pages_move_kernel, dim3(table_wgs + copy_grid(copy_items(a, a.num_pages / 2))), dim3(kCopyThreads), 0, s, a,
+                       tables, std::max(entries, 1), stride, n_entries, ws, (int32_t)table_wgs);
     return hipGetLastError();
 }
 
