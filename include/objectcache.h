@@ -308,7 +308,8 @@ size_t oc_kv4_attention_workspace_bytes(const oc_layout *layout, int64_t prefix_
 
 /* oc_suffix_prefill_layer over a prefix held in 4 bits: the prefix's K and V
  * are the values that its codes stand for (exact in bfloat16), the suffix's are
- * k_new and v_new as they are.  Same arguments, workspace rules, rounding and
+ * k_new and v_new as they are.  Same arguments, workspace rules (nothing in it
+ * needs to start at zero; calls that may run at once need one each), rounding and
  * asynchrony.  An infinity or NaN in a k_new or v_new row reaches no row of a
  * token before it. */
 int oc_kv4_suffix_prefill_layer(const void *q, const void *k_new, const void *v_new, int64_t suffix_tokens,
@@ -342,8 +343,8 @@ size_t oc_kv4_decode_workspace_bytes(const oc_layout *layout, int64_t batch, int
  * num_tokens[i] / page_size + 1 are used; the page that receives the token must
  * be no other table's (oc_kv_pages_fork sees to that).  batch == 0 is not an
  * error; batch <= 65535.  workspace: device, at least
- * oc_kv4_decode_workspace_bytes(), 256-byte aligned.  Asynchronous on
- * `stream`. */
+ * oc_kv4_decode_workspace_bytes(), 256-byte aligned, as for
+ * oc_kv4_suffix_prefill_layer.  Asynchronous on `stream`. */
 int oc_kv4_decode_layer(const void *q, const void *k_new, const void *v_new, int64_t batch, oc_kv_pool *kv_pool,
                         const oc_page_tables *tables, const int32_t *num_tokens, int64_t max_tokens, int32_t layer,
                         void *out, void *workspace, size_t workspace_bytes, void *stream);

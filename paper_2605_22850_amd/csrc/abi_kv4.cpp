@@ -319,6 +319,17 @@ static int pages_compact(oc_kv_pool *pool, int32_t bits, int32_t *counts, const 
     return OC_OK;
 }
 
+// What a size function returns: 0 where the layout or sizes are refused.
+template <class F>
+static size_t bytes_of(const oc_layout *layout, F &&body) noexcept {
+    size_t n = 0;
+    const int rc = guarded([&]() -> int {
+        clear_error();
+        return layout ? body(&n) : fail(OC_EINVAL, "layout is NULL");
+    });
+    return rc ? 0 : n;
+}
+
 }  // namespace oc
 
 using namespace oc;
@@ -326,12 +337,14 @@ using namespace oc;
 extern "C" {
 
 size_t oc_kv4_pool_bytes(const oc_layout *layout) {
-    clear_error();
-    if (!layout) {
-        fail(OC_EINVAL, "layout is NULL");
-        return 0;
-    }
-    return check_kv4_layout(*layout) ? 0 : (size_t)(2 * layout->num_layers * layout->num_pages * kv4_page_bytes(*layout));
+    return bytes_of(layout, [&](size_t *n) {
+        const int rc = check_kv4_layout(*layout);
+        // 2 * L * P pages of less than 2^31 bytes
+        if (!rc && layout->num_pages > INT64_MAX / 2 / layout->num_layers / kv4_page_bytes(*layout))
+            return fail(OC_ERANGE, "a pool of more than 2^63 bytes");
+        *n = rc ? 0 : (size_t)(2 * layout->num_layers * layout->num_pages * kv4_page_bytes(*layout));
+        return rc;
+    });
 }
 
 int oc_kv4_layer_ingest(const oc_staging *staging, const oc_block_table *block_table, oc_kv_pool *kv_pool, int32_t layer,
@@ -352,13 +365,12 @@ int oc_kv4_layer_gather(const oc_block_table *block_table, const oc_kv_pool *kv_
 }
 
 size_t oc_kv4_attention_workspace_bytes(const oc_layout *layout, int64_t prefix_tokens, int64_t suffix_tokens) {
-    clear_error();
-    if (!layout) {
-        fail(OC_EINVAL, "layout is NULL");
-        return 0;
-    }
-    Kv4Plan p;
-    return plan_kv4_attention(*layout, prefix_tokens, suffix_tokens, &p) ? 0 : p.total;
+    return bytes_of(layout, [&](size_t *n) {
+        Kv4Plan p;
+        const int rc = plan_kv4_attention(*layout, prefix_tokens, suffix_tokens, &p);
+        *n = rc ? 0 : p.total;
+        return rc;
+    });
 }
 
 int oc_kv4_suffix_prefill_layer(const void *q, const void *k_new, const void *v_new, int64_t suffix_tokens,
@@ -371,13 +383,12 @@ int oc_kv4_suffix_prefill_layer(const void *q, const void *k_new, const void *v_
 }
 
 size_t oc_kv4_decode_workspace_bytes(const oc_layout *layout, int64_t batch, int64_t max_tokens) {
-    clear_error();
-    if (!layout) {
-        fail(OC_EINVAL, "layout is NULL");
-        return 0;
-    }
-    Kv4Plan p;
-    return plan_kv4_decode(*layout, batch, max_tokens, &p) ? 0 : p.total;
+    return bytes_of(layout, [&](size_t *n) {
+        Kv4Plan p;
+        const int rc = plan_kv4_decode(*layout, batch, max_tokens, &p);
+        *n = rc ? 0 : p.total;
+        return rc;
+    });
 }
 
 int oc_kv4_decode_layer(const void *q, const void *k_new, const void *v_new, int64_t batch, oc_kv_pool *kv_pool,
@@ -409,12 +420,11 @@ int oc_kv_pages_release(const oc_block_table *block_table, const oc_layout *layo
 }
 
 size_t oc_kv_pages_workspace_bytes(const oc_layout *layout) {
-    clear_error();
-    if (!layout) {
-        fail(OC_EINVAL, "layout is NULL");
-        return 0;
-    }
-    return check_pages_layout(*layout) ? 0 : pages_workspace_bytes(layout->num_pages);
+    return bytes_of(layout, [&](size_t *n) {
+        const int rc = check_pages_layout(*layout);
+        *n = rc ? 0 : pages_workspace_bytes(layout->num_pages);
+        return rc;
+    });
 }
 
 int oc_kv_pages_compact(oc_kv_pool *kv_pool, int32_t bits, int32_t *page_counts, const oc_page_tables *tables,

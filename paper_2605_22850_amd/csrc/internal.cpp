@@ -2,7 +2,7 @@
 // part of the C ABI.
 #include <algorithm>
 
-#include "common.hpp"
+#include "kv4.hpp"
 
 using namespace oc;
 
@@ -78,6 +78,20 @@ void oc_internal_registers(int32_t tile_rows, int32_t head_dim, int pow2_ingest,
     p.d = head_dim;
     *attention = attention_registers(p);
     *ingest = ingest_registers(pow2_ingest != 0);
+}
+
+// The plan of one request's attention over a 4-bit prefix, or of a decode call of
+// `batch` requests (suffix_tokens then counts for nothing): out = tile rows, row
+// tiles, key units, splits, units per split.  An oc_status.
+int oc_internal_kv4_plan(const oc_layout *layout, int64_t batch, int64_t prefix_tokens, int64_t suffix_tokens,
+                         int64_t *out) {
+    Kv4Plan p;
+    const int rc = batch ? plan_kv4_decode(*layout, batch, prefix_tokens, &p)
+                         : plan_kv4_attention(*layout, prefix_tokens, suffix_tokens, &p);
+    if (rc) return rc;
+    const int64_t v[5] = {p.row_tile, p.m_tiles, p.n_units, p.n_split, p.units_per_split};
+    std::copy(v, v + 5, out);
+    return OC_OK;
 }
 
 }  // extern "C"

@@ -50,23 +50,28 @@ struct Kv4Params {
 // unit of one row tile, not 99.)
 __device__ __forceinline__ int v4_swz(int r) { return ((r & 3) << 1) | ((r >> 2) & 1); }
 
-// codes and scale byte of this lane's quarter of its key's row, K's or V's
+// Codes and scale byte of this lane's quarter of its key's row, K's or V's.  ONCE:
+// nothing else reads the page, so its codes bypass the caches (decode of eight requests
+// of 32K tokens: 58 -> 52.5 us; a lone request's 35 MB, which a benchmark finds in the
+// caches again, gains nothing).
 template <int D>
 struct Piece4 {
     uint32_t c[D / 32], b;
 };
 
-template <int D>
+template <int D, bool ONCE>
 __device__ __forceinline__ Piece4<D> load_piece4(const unsigned char *page, uint32_t code_at, uint32_t scale_at) {
     Piece4<D> r;
     if constexpr (D == 128) {
-        const u32x4 v = *reinterpret_cast<const u32x4 *>(page + code_at);
+        const u32x4 *from = reinterpret_cast<const u32x4 *>(page + code_at);
+        const u32x4 v = ONCE ? __builtin_nontemporal_load(from) : *from;
 #pragma unroll
         for (int i = 0; i < 4; ++i) r.c[i] = v[i];
     } else {
-        const uint2 v = *reinterpret_cast<const uint2 *>(page + code_at);
-        r.c[0] = v.x;
-        r.c[1] = v.y;
+        const uint64_t *from = reinterpret_cast<const uint64_t *>(page + code_at);
+        const uint64_t v = ONCE ? __builtin_nontemporal_load(from) : *from;
+        r.c[0] = (uint32_t)v;
+        r.c[1] = (uint32_t)(v >> 32);
     }
     r.b = page[scale_at];
     return r;
@@ -267,8 +272,8 @@ __global__ __launch_bounds__(NW4 * 64, NR == 1 ? 4 : 2) void kv4_ways_kernel(Kv4
             const unsigned char *const base = reinterpret_cast<const unsigned char *>(
                 (uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)at, from) |
                 (uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)(at >> 32), from) << 32);
-            k[i] = load_piece4<D>(base, ca[i], sa[i]);
-            v[i] = load_piece4<D>(base + kv_step, ca[i], sa[i]);
+            k[i] = load_piece4<D, DECODE>(base, ca[i], sa[i]);
+            v[i] = load_piece4<D, DECODE>(base + kv_step, ca[i], sa[i]);
         }
     };
     auto unit = [&](int n, int u, Piece4<D> (&k)[2], Piece4<D> (&v)[2]) {
@@ -973,6 +978,7 @@ int plan_kv4_decode(const oc_layout &l, int64_t batch, int64_t max_tokens, Kv4Pl
     p.n_units = (int)(((max_tokens + PAGE - 1) / PAGE + 1) / 2);
     const int64_t pairs = batch * p.nkv;
     if (pairs > OC_MAX_GRID_ITEMS / THREADS) return fail(OC_ERANGE, "attention grid of more than 2^32 work-items");
+    if (p.m_tiles > 65535) return fail(OC_ERANGE, "more than 2^20 query heads to a KV head");
     const int64_t fill = std::max<int64_t>(1, 256 / (pairs * p.m_tiles));
     int64_t ns = 1;
     if (p.n_units > 3 * NW4) ns = (std::max<int64_t>(fill, (p.n_units + 159) / 160) + fill - 1) / fill * fill;

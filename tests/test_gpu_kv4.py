@@ -5,6 +5,7 @@ import numpy as np
 import pytest
 
 from tests import kv4_ref as ref
+from tests.kv4_cases import BY_PLAN, RAGGED_256
 from tests.gpu_util import require_gpu
 
 pytestmark = pytest.mark.gpu
@@ -187,19 +188,13 @@ def test_attention(nq, nkv, d, tp, ts):
     c.check(c.run())
 
 
-LONG = [
-    # keys split over workgroups, many row tiles, long suffixes
-    (32, 8, 128, 4096, 128), (8, 2, 64, 9001, 2), (32, 8, 128, 8005, 300), (64, 8, 128, 3001, 97), (32, 4, 64, 5003, 200),
-    (8, 1, 128, 20003, 1), (8, 1, 128, 33, 2000), (32, 8, 64, 2005, 700), (24, 3, 128, 4001, 200), (4, 4, 128, 0, 1500),
-    (8, 1, 128, 15001, 700), (16, 2, 64, 10007, 900),
-]
-
-
-@pytest.mark.parametrize("nq,nkv,d,tp,ts", LONG)
-def test_long_attention(nq, nkv, d, tp, ts):
+@pytest.mark.parametrize("nq,nkv,d,tp,ts", [s for shapes in BY_PLAN.values() for s in shapes] + RAGGED_256)
+def test_every_kernel(nq, nkv, d, tp, ts):
+    """Row tiles of each size, keys whole and split over workgroups."""
     c = Case(nq, nkv, d, tp, ts)
     out = c.run()
-    rows = sorted({0, 1 % ts, ts // 3, ts // 2, ts - 1})
+    grp = nq // nkv
+    rows = sorted({0, 1 % ts, 15 // grp % ts, 16 // grp % ts, 256 // grp % ts, ts // 3, ts // 2, ts - 1})
     c.check(out, rows)
     assert bool(c.torch.isfinite(out.float()).all())
     # the same call again, into another workspace: the same bits
@@ -395,6 +390,41 @@ def test_decode_long_and_short_together():
     b.check(first)
     import torch
     assert torch.equal(b.run(), first)          # the token is stored again where it stood
+
+
+def test_decode_two_calls_at_once():
+    """Two batches of one pool on two streams, each with its workspace and tables."""
+    import torch
+    bs = [Batch(32, 8, 128, [3000, 40, -1, 700], seed=s) for s in range(2)]
+    want = [b.run() for b in bs]
+    torch.cuda.synchronize()
+    outs = []
+    for b in bs:
+        s = torch.cuda.Stream()
+        s.wait_stream(torch.cuda.current_stream())
+        with torch.cuda.stream(s):
+            outs.append(b.run())
+    torch.cuda.synchronize()
+    for b, a, o in zip(bs, want, outs):
+        assert torch.equal(a, o)
+        b.check(o)
+
+
+def test_decode_many_requests():
+    """More requests than a workgroup has threads, of a few tokens each."""
+    rng = np.random.default_rng(8)
+    b = Batch(4, 2, 64, rng.integers(-1, 40, 600).tolist(), room=3)
+    got = host16(b.run())
+    for i in rng.permutation(600)[:60]:
+        n = b.lengths[i]
+        if n < 0:
+            assert (got[i] == 0x4040).all()
+            continue
+        k, v = (np.concatenate((b.pool.get(1, kv, b.tables[i], n), ref.bf16_to_f64(x[i:i + 1])))
+                for kv, x in ((0, b.k), (1, b.v)))
+        ref.assert_rows_close(got[i:i + 1], *ref.attention(ref.bf16_to_f64(b.q[i:i + 1]), k, v, [n + 1]))
+    b.append()
+    assert np.array_equal(b.d_pool.cpu().numpy(), b.pool.raw)
 
 
 def test_decode_special_tokens():

@@ -10,6 +10,7 @@ import pytest
 import paper_2605_22850_amd as oc
 from paper_2605_22850_amd import _lib as L
 from tests import kv4_ref as ref
+from tests.kv4_cases import BY_PLAN, RAGGED_256
 
 FAKE = 1 << 20            # aligned non-null "device" address; never dereferenced
 BIG = 1 << 40
@@ -77,9 +78,53 @@ def test_sizes_of_unsupported_layouts():
         assert oc.lib().oc_kv4_decode_workspace_bytes(lay, b, most) == 0
     assert oc.lib().oc_kv4_attention_workspace_bytes(lay, 0, 1) >= 256
     assert oc.lib().oc_kv4_decode_workspace_bytes(lay, 1, 0) >= 256
+    # a pool whose size has no 64-bit number
+    assert oc.lib().oc_kv4_pool_bytes(ctypes.byref(_layout(num_layers=1 << 30, num_pages=1 << 60))) == 0
     for f in ("oc_kv4_pool_bytes", "oc_kv_pages_workspace_bytes"):
         assert getattr(oc.lib(), f)(None) == 0
     assert oc.oc_kv_pages_workspace_bytes(oc.Layout(1, 1, 1, 32, 8, 8, 9)) >= (9 + 2 * 4) * 4
+
+
+# ---- plans ------------------------------------------------------------------
+
+def plan(nq, nkv, d, tp, ts, batch=0):
+    """Tile rows, row tiles, key units, splits, units per split."""
+    lay, out = L.c_layout(1, nq, nkv, d, 16, 16, 1 << 40), (c_int64 * 5)()
+    assert oc.lib().oc_internal_kv4_plan(ctypes.byref(lay), c_int64(batch), c_int64(tp), c_int64(ts), out) == 0
+    return list(out)
+
+
+@pytest.mark.parametrize("want", BY_PLAN)
+def test_every_kernel_has_its_shapes(want):
+    for shape in BY_PLAN[want]:
+        tile, _, _, splits, _ = plan(*shape)
+        assert (tile, shape[2], "none" if splits == 1 else "few" if splits <= 8 else "many") == want, shape
+
+
+def test_ragged_prefixes_reach_the_large_tiles():
+    assert {plan(*s)[0] for s in RAGGED_256} == {256}
+
+
+def test_plans_cover_rows_and_keys():
+    rng = np.random.default_rng(2)
+    for _ in range(2000):
+        nkv = int(rng.integers(1, 17))
+        nq, d = nkv * int(rng.integers(1, 20)), int(rng.choice([64, 128]))
+        tp, ts = int(np.exp(rng.uniform(0, 11.5))) - 1, int(np.exp(rng.uniform(0, 9)))
+        tile, m_tiles, units, splits, per = plan(nq, nkv, d, tp, ts)
+        rows = ts * nq // nkv
+        assert (m_tiles - 1) * tile < rows <= m_tiles * tile
+        assert (splits - 1) * per < units <= splits * per
+        pages = (-(-tp // 16), -(-ts // 16))
+        assert units == (-(-sum(pages) // 4) if tile == 256 else -(-pages[0] // 2) + -(-ts // 32))
+        need = oc.oc_kv4_attention_workspace_bytes(oc.Layout(1, nq, nkv, d, 16, 16, 8), tp, ts)
+        assert need >= (splits * nkv * rows * (d + 2) * 4 if splits > 1 else 256)
+        batch = int(rng.integers(1, 300))
+        tile, m_tiles, units, splits, per = plan(nq, nkv, d, tp, 1, batch)
+        assert m_tiles * tile >= nq // nkv and units == -(-(-(-tp // 16)) // 2) and per % 8 == 0
+        assert splits * per >= units and (splits == 1 or (splits - 1) * per < units)
+        need = oc.oc_kv4_decode_workspace_bytes(oc.Layout(1, nq, nkv, d, 16, 16, 8), batch, tp)
+        assert need >= (splits * batch * nq * (d + 2) * 4 if splits > 1 else 256)
 
 
 # ---- refusals ---------------------------------------------------------------
