@@ -341,8 +341,10 @@ size_t oc_kv4_decode_workspace_bytes(const oc_layout *layout, int64_t batch, int
  * written.  Lengths above max_tokens are taken as max_tokens.  Every table needs
  * max_tokens / page_size + 1 entries, of which the first
  * num_tokens[i] / page_size + 1 are used; the page that receives the token must
- * be no other table's (oc_kv_pages_fork sees to that).  batch == 0 is not an
- * error; batch <= 65535.  workspace: device, at least
+ * be no other table's (oc_kv_pages_fork sees to that).  An id outside [0, P), as
+ * a fork or take without enough pages leaves it, touches nothing outside the pool:
+ * the token is not appended, or page 0 is read in its place (and that row means
+ * nothing).  batch == 0 is not an error; batch <= 65535.  workspace: device, at least
  * oc_kv4_decode_workspace_bytes(), 256-byte aligned, as for
  * oc_kv4_suffix_prefill_layer.  Asynchronous on `stream`. */
 int oc_kv4_decode_layer(const void *q, const void *k_new, const void *v_new, int64_t batch, oc_kv_pool *kv_pool,
@@ -378,7 +380,8 @@ int oc_kv_pages_copy(oc_kv_pool *kv_pool, int32_t bits, const int32_t *src_pages
  * the last page is partly filled, a page of the child's own (the lowest free
  * ones, ascending by child, with a count of 1) into which all of the parent's is
  * copied, so that each may append to its own.  With too few free pages *status is
- * OC_ENOMEM, the children's last entries are -1, and nothing else changes. */
+ * OC_ENOMEM, the children's last entries are -1, and nothing else changes.
+ * The parent's table must not overlap a child's (OC_EINVAL). */
 int oc_kv_pages_fork(oc_kv_pool *kv_pool, int32_t bits, const oc_block_table *parent, const oc_page_tables *children,
                      int64_t num_children, int32_t *page_counts, int32_t *status, void *stream);
 

@@ -1,5 +1,7 @@
 // C entry points of the 4-bit paged cache and of the page operations: argument
 // validation, then launch.  Nothing is enqueued unless every check passes.
+#include <algorithm>
+#include <cstdlib>
 #include <string>
 
 #include "kv4.hpp"
@@ -195,6 +197,7 @@ static int decode(const void *q, const void *k_new, const void *v_new, int64_t b
     a.table_stride = tables->stride;
     a.num_tokens = num_tokens;
     a.max_tokens = (int32_t)max_tokens;
+    a.num_pages = (int32_t)std::min<int64_t>(l.num_pages, INT32_MAX);      // ids are 32-bit
     OC_HIP(launch_kv4_attention(p, a, static_cast<hipStream_t>(stream)));
     return OC_OK;
 }
@@ -260,6 +263,15 @@ static int pages_copy(oc_kv_pool *pool, int32_t bits, const int32_t *src, const 
     return OC_OK;
 }
 
+// Do the first `need` entries of `pages` meet those of one of the n tables?  (n, need > 0)
+static bool overlaps(const int32_t *pages, const oc_page_tables &t, int64_t n, int64_t need) {
+    const int64_t off = (int64_t)((intptr_t)pages - (intptr_t)t.pages) / 4;
+    if (off <= -need) return false;
+    // the table that begins at or before `pages`, and the next
+    const int64_t c = n > 1 ? std::max<int64_t>(0, std::min(off / t.stride, n - 1)) : 0;
+    return std::abs(off - c * t.stride) < need || (c + 1 < n && (c + 1) * t.stride - off < need);
+}
+
 static int pages_fork(oc_kv_pool *pool, int32_t bits, const oc_block_table *parent, const oc_page_tables *children,
                       int64_t n, int32_t *counts, int32_t *status, void *stream) {
     clear_error();
@@ -274,6 +286,8 @@ static int pages_fork(oc_kv_pool *pool, int32_t bits, const oc_block_table *pare
     if ((rc = check_tables(children, n, need))) return rc;
     if (!counts || !status) return fail(OC_EINVAL, "NULL page_counts or status");
     if (need > 0 && n > 0 && (rc = check_pool_base(pool))) return rc;
+    if (need > 0 && n > 0 && overlaps(parent->pages, *children, n, need))
+        return fail(OC_EINVAL, "the parent's table is among the children's");
     a.counts = counts;
     a.status = status;
     const bool part = n > 0 && parent->num_tokens % l.page_size != 0;

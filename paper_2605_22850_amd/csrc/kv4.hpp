@@ -62,7 +62,7 @@ struct Kv4AttnArgs {
     uint16_t *out;
     unsigned char *ws;
     int64_t page_bytes;
-    int32_t code_bytes;
+    int32_t code_bytes, num_pages;
 };
 int plan_kv4_attention(const oc_layout &l, int64_t Tp, int64_t Ts, Kv4Plan *p);
 int plan_kv4_decode(const oc_layout &l, int64_t batch, int64_t max_tokens, Kv4Plan *p);

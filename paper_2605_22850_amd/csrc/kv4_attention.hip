@@ -25,7 +25,7 @@ struct Kv4Params {
     float2 *ml_part;
     uint16_t *out;
     int64_t page_bytes, table_stride;
-    int code_bytes, Tp, Ts, rows, nq, nkv, grp, m_tiles, n_split, n_groups, n_units, units_per_split, max_tokens, batch;
+    int code_bytes, num_pages, Tp, Ts, rows, nq, nkv, grp, m_tiles, n_split, n_groups, n_units, units_per_split, max_tokens, batch;
     float scale_log2;
 };
 
@@ -155,9 +155,12 @@ __global__ __launch_bounds__(NW4 * 64, NR == 1 ? 4 : 2) void kv4_ways_kernel(Kv4
             uint32_t sb;
             const uint32_t codes = kv4_encode8(x, &sb);
             const int slot = Tp % PAGE;
-            unsigned char *page = (kv ? p.pool_v : p.pool_k) + (int64_t)pages[Tp / PAGE] * page_bytes;
-            *reinterpret_cast<uint32_t *>(page + head_codes + slot * (D / 2) + i * 4) = codes;
-            if ((i & 3) == 0) page[head_scales + slot * (D / 32) + i / 4] = (unsigned char)sb;
+            const int32_t id = pages[Tp / PAGE];
+            if ((uint32_t)id < (uint32_t)p.num_pages) {
+                unsigned char *page = (kv ? p.pool_v : p.pool_k) + (int64_t)id * page_bytes;
+                *reinterpret_cast<uint32_t *>(page + head_codes + slot * (D / 2) + i * 4) = codes;
+                if ((i & 3) == 0) page[head_scales + slot * (D / 32) + i / 4] = (unsigned char)sb;
+            }
         }
     }
 
@@ -245,7 +248,10 @@ __global__ __launch_bounds__(NW4 * 64, NR == 1 ? 4 : 2) void kv4_ways_kernel(Kv4
     auto load_ids = [&](int u) {
         int pg = 2 * (u + (lane >> 1) * NW4) + (lane & 1);
         if (pg > n_pre_pages - 1) pg = n_pre_pages - 1;
-        at = reinterpret_cast<uint64_t>(p.pool_k) + (uint64_t)((int64_t)pages[pg] * page_bytes);
+        int32_t id = pages[pg];
+        // (a table of the decode form may hold what a fork or take left that found no page)
+        if (DECODE && (uint32_t)id >= (uint32_t)p.num_pages) id = 0;
+        at = reinterpret_cast<uint64_t>(p.pool_k) + (uint64_t)((int64_t)id * page_bytes);
     };
     auto code_at = [&](int slot) { return head_codes + slot * (D / 2) + g * (D / 8); };
     auto scale_at = [&](int slot) { return head_scales + slot * (D / 32) + g * D / 128; };
@@ -1010,6 +1016,7 @@ static Kv4Params make_params(const Kv4Plan &pl, const Kv4AttnArgs &a) {
     p.page_bytes = a.page_bytes;
     p.table_stride = a.table_stride;
     p.code_bytes = a.code_bytes;
+    p.num_pages = a.num_pages;
     p.Tp = (int)pl.Tp;
     p.Ts = (int)pl.Ts;
     p.rows = (int)pl.rows;

@@ -447,6 +447,22 @@ def test_decode_lengths_above_max_tokens():
     b.check(b.run(most=64))
 
 
+def test_decode_page_ids_outside_the_pool():
+    """As a fork or take without pages leaves them: a token without a page is not appended, and where a prefix
+    names none page 0 is read; the other rows are as ever, and nothing else is written."""
+    b = Batch(4, 2, 64, [40, 96, 33, 16])
+    b.d_tables[1, 6], b.d_tables[3, 1], b.d_tables[2, 0] = -1, b.lay.num_pages, -5
+    got = host16(b.run())
+    for i in (0, 1, 3):
+        n = b.lengths[i]
+        k, v = (np.concatenate((b.pool.get(1, kv, b.tables[i], n), ref.bf16_to_f64(x[i:i + 1])))
+                for kv, x in ((0, b.k), (1, b.v)))
+        ref.assert_rows_close(got[i:i + 1], *ref.attention(ref.bf16_to_f64(b.q[i:i + 1]), k, v, [n + 1]))
+    b.lengths = [40, -1, 33, -1]
+    b.append()
+    assert np.array_equal(b.d_pool.cpu().numpy(), b.pool.raw)
+
+
 def test_decode_captured_while_requests_grow():
     """One captured call, replayed as the lengths grow on the device, with a place that empties."""
     import torch

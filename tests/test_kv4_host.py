@@ -261,6 +261,21 @@ def test_pages_refusals():
     assert compact(pool=ctypes.byref(L.c_kv_pool(None, lay))) == L.OC_EINVAL
 
 
+def test_a_fork_refuses_the_parents_table_among_the_childrens():
+    lib, lay = oc.lib(), _layout()
+    kp, word = L.c_kv_pool(FAKE, lay), 4
+
+    def fork(parent, n, tokens, stride):
+        tabs = L.c_page_tables(FAKE, n, 16, stride)
+        return lib.oc_kv_pages_fork(ctypes.byref(kp), 16, ctypes.byref(_table(16, tokens, FAKE + word * parent)),
+                                    ctypes.byref(tabs), n, FAKE, FAKE, None)
+    for n, stride in ((1, 16), (1, 0), (4, 16), (4, 40)):
+        for c in range(n):
+            for near in (-9, 0, 9):                     # ten entries each
+                assert fork(c * stride + near, n, 150, stride) == L.OC_EINVAL, (n, stride, c, near)
+                assert b"parent" in lib.oc_last_error()
+
+
 # ---- marshalling ------------------------------------------------------------
 
 KP, BT, ST, PT, LAY = (POINTER(t) for t in (L.c_kv_pool, L.c_block_table, L.c_staging, L.c_page_tables, L.c_layout))
