@@ -94,4 +94,15 @@ int oc_internal_kv4_plan(const oc_layout *layout, int64_t batch, int64_t prefix_
     return OC_OK;
 }
 
+// The key ranges of a decode: out[0] wanted (0: no list, n_split of each request),
+// out[1] at most of all requests.
+int oc_internal_kv4_ranges(const oc_layout *layout, int64_t batch, int64_t max_tokens, int64_t *out) {
+    Kv4Plan p;
+    const int rc = plan_kv4_decode(*layout, batch, max_tokens, &p);
+    if (rc) return rc;
+    out[0] = p.ranges;
+    out[1] = p.n_ranges;
+    return OC_OK;
+}
+
 }  // extern "C"

@@ -50,6 +50,7 @@ struct Kv4Plan {
     int32_t row_tile, m_tiles;
     int32_t n_split, n_units, units_per_split;    // key units of two pages, prefix then suffix
     int32_t batch;                // 0: one request's suffix; else requests with a token each
+    int32_t ranges, n_ranges;     // decode: key ranges wanted of all requests (0: n_split of each), and at most
     size_t off_ml, total;         // workspace: partial rows, then their (max, sum) pairs
 };
 struct Kv4AttnArgs {

@@ -25,8 +25,8 @@ struct Kv4Params {
     float2 *ml_part;
     uint16_t *out;
     int64_t page_bytes, table_stride;
-    int code_bytes, num_pages, Tp, Ts, rows, nq, nkv, grp, m_tiles, n_split, n_groups, n_units, units_per_split, max_tokens, batch;
-    float scale_log2;
+    int code_bytes, num_pages, Tp, Ts, rows, nq, nkv, grp, m_tiles, n_split, n_groups, n_units, units_per_split, max_tokens, batch, ranges;
+    float scale_log2, per_range;
 };
 
 // ---------------------------------------------------------------------------
@@ -90,6 +90,108 @@ __device__ __forceinline__ float row_sum(float x) {
     return x + __shfl_xor(x, 32);
 }
 
+// ---- decode: which key range of which request a workgroup has ----
+// Sum of x over this lane and the ones before it.
+__device__ __forceinline__ uint32_t wave_scan(uint32_t x) {
+    x += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x111, 0xF, 0xF, false);    // row_shr by 1, 2, 4, 8
+    x += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x112, 0xF, 0xF, false);
+    x += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x114, 0xF, 0xF, false);
+    x += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x118, 0xF, 0xF, false);
+    x += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x142, 0xA, 0xF, false);    // row_bcast 15, 31
+    x += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x143, 0xC, 0xF, false);
+    return x;
+}
+
+// Tokens cached for request b; -1: an empty place, or none.
+__device__ __forceinline__ int tokens_of(const Kv4Params &p, int b) {
+    if (b >= p.batch) return -1;
+    const int t = p.num_tokens[b];
+    return t < 0 ? -1 : t > p.max_tokens ? p.max_tokens : t;
+}
+__device__ __forceinline__ int units_of(int tokens) { return ((tokens + PAGE - 1) / PAGE + 1) / 2; }
+
+// The key ranges of a decode over requests whose lengths only the device knows:
+// every request's whole ones of `per` units first, then what is left of each, those of
+// more than half a range before the others, so that what starts last is short.  How
+// many of each kind there are is one number, ten bits each.  Every wavefront works
+// the list out by itself, PER requests to a lane.
+__device__ __forceinline__ int kind_of(uint32_t n, int kind) { return (int)(n >> 10 * kind & 1023u); }
+__device__ __forceinline__ uint32_t lane_of(uint32_t x, int lane) { return (uint32_t)__builtin_amdgcn_readlane((int)x, lane); }
+
+template <int PER>
+struct RangeList {
+    int per;                           // units of a range
+    int tokens[PER];                   // this lane's requests
+    uint32_t n[PER], upto, all;        // their ranges; those of this lane and the ones before; of all
+
+    // units in all are below 2^24, so a float holds them
+    __device__ __forceinline__ RangeList(const Kv4Params &p, int lane) {
+        uint32_t sum = 0;
+#pragma unroll
+        for (int i = 0; i < PER; ++i) tokens[i] = tokens_of(p, lane * PER + i);
+#pragma unroll
+        for (int i = 0; i < PER; ++i) sum += tokens[i] > 0 ? units_of(tokens[i]) : 0;
+        const uint32_t units = lane_of(wave_scan(sum), 63);
+        per = ((int)((float)units * p.per_range) + NW4) / NW4 * NW4;     // at least units / ranges
+        if (per < p.units_per_split) per = p.units_per_split;
+        const float inv = __builtin_amdgcn_rcpf((float)per);
+        upto = 0;
+#pragma unroll
+        for (int i = 0; i < PER; ++i) {
+            const int u = tokens[i] > 0 ? units_of(tokens[i]) : 0;
+            int whole = (int)((float)u * inv), left = u - whole * per;   // off by one at most
+            if (left < 0) --whole, left += per;
+            if (left >= per) ++whole, left -= per;
+            n[i] = (uint32_t)whole | (left > per / 2 ? 1u << 10 : left || tokens[i] == 0 ? 1u << 20 : 0u);
+            upto += n[i];
+        }
+        upto = wave_scan(upto);
+        all = lane_of(upto, 63);
+    }
+    // Range x of the list: its request, that one's tokens, and which of its ranges; false past the last.
+    __device__ __forceinline__ bool find(int x, int &b, int &t, int &split) const {
+        int kind = 0;
+        while (kind < 3 && x >= kind_of(all, kind)) x -= kind_of(all, kind++);
+        if (kind == 3) return false;
+        const int at = __ffsll((unsigned long long)__ballot(kind_of(upto, kind) > x)) - 1;
+        uint32_t own = 0;
+#pragma unroll
+        for (int i = 0; i < PER; ++i) own += n[i];
+        x -= kind_of(lane_of(upto - own, at), kind);
+        int in = 0;
+#pragma unroll
+        for (int i = 0; i + 1 < PER; ++i) {
+            const int here = kind_of(lane_of(n[i], at), kind);
+            if (in == i && x >= here) x -= here, ++in;
+        }
+        b = at * PER + in;
+#pragma unroll
+        for (int i = 0; i < PER; ++i)
+            if (in == i) {
+                t = (int)lane_of((uint32_t)tokens[i], at);
+                split = kind ? kind_of(lane_of(n[i], at), 0) : x;
+            }
+        return true;
+    }
+    // Request b's ranges: how many, its first whole one in the list, and its last one.
+    __device__ __forceinline__ int of_request(int b, int &first, int &last) const {
+        const int at = b / PER, in = b % PER;
+        uint32_t before = upto, mine = 0;
+#pragma unroll
+        for (int i = 0; i < PER; ++i) {
+            if (i >= in) before -= n[i];
+            if (i == in) mine = n[i];
+        }
+        before = lane_of(before, at);
+        mine = lane_of(mine, at);
+        const int whole = kind_of(mine, 0), kind = kind_of(mine, 1) ? 1 : kind_of(mine, 2) ? 2 : 0;
+        first = kind_of(before, 0);
+        last = kind == 0 ? first + whole - 1
+                         : kind_of(all, 0) + (kind == 2 ? kind_of(all, 1) : 0) + kind_of(before, kind);
+        return whole + (kind > 0);
+    }
+};
+
 template <int D, int NR, int PF, bool DECODE>
 __global__ __launch_bounds__(NW4 * 64, NR == 1 ? 4 : 2) void kv4_ways_kernel(Kv4Params p) {
     constexpr int ROWS = 16 * NR, NDS = D / 32, NT = D / 16;
@@ -100,28 +202,37 @@ __global__ __launch_bounds__(NW4 * 64, NR == 1 ? 4 : 2) void kv4_ways_kernel(Kv4
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int c = lane & 15, g = lane >> 4;
 
-    int b = 0, h, mt, split;
+    int b = 0, h, mt, split, range, per = p.units_per_split, Tp = p.Tp;
     if (DECODE) {
-        // first splits, which every request has, come first, and neighbours are of different
-        // heads and requests: no XCD gets the long ones
-        int i = (int)blockIdx.x;
-        const int pairs = p.batch * p.nkv;
-        split = i / pairs;
-        i -= split * pairs;
-        b = i / p.nkv;
-        h = i - b * p.nkv;
+        // neighbours are of different heads: no XCD gets the long requests
+        range = (int)blockIdx.x / p.nkv;
+        h = (int)blockIdx.x - range * p.nkv;
         mt = (int)blockIdx.y;
+        if (p.ranges) {
+            bool some;
+            if (p.batch <= 64) {
+                const RangeList<1> list(p, lane);
+                per = list.per;
+                some = list.find(range, b, Tp, split);
+            } else {
+                const RangeList<2> list(p, lane);
+                per = list.per;
+                some = list.find(range, b, Tp, split);
+            }
+            if (!some) return;                            // fewer ranges than workgroups
+        } else {
+            // first splits, which every request has, come first
+            split = range / p.batch;
+            b = range - split * p.batch;
+            range = b * p.n_split + split;
+            Tp = tokens_of(p, b);
+            if (Tp < 0) return;                           // an empty place of the batch
+        }
     } else {
         mt = (int)blockIdx.x / p.n_groups;
         const int gamma = (int)blockIdx.x - mt * p.n_groups;
         h = gamma / p.n_split;
-        split = gamma - h * p.n_split;
-    }
-    int Tp = p.Tp;
-    if (DECODE) {
-        Tp = p.num_tokens[b];
-        if (Tp < 0) return;                               // an empty place of the batch
-        if (Tp > p.max_tokens) Tp = p.max_tokens;
+        split = range = gamma - h * p.n_split;
     }
     const int Ts = p.Ts, rows = p.rows, grp = p.grp, nq = p.nq, nkv = p.nkv;
     const int n_pre_pages = (Tp + PAGE - 1) / PAGE, n_pre = (n_pre_pages + 1) / 2;
@@ -135,11 +246,11 @@ __global__ __launch_bounds__(NW4 * 64, NR == 1 ? 4 : 2) void kv4_ways_kernel(Kv4
     int row_hi = (mt + 1) * ROWS - 1;
     if (row_hi > rows - 1) row_hi = rows - 1;
     const int n_units = n_pre + row_hi / grp / UNIT4 + 1;
-    const int u0 = split * p.units_per_split;
-    int u1 = u0 + p.units_per_split, n_used = p.n_split;
+    const int u0 = split * per;
+    int u1 = u0 + per, n_used = p.n_split;
     if (DECODE) {
         // the prefix's units are split, and the token's own goes with the last of them
-        n_used = n_pre > p.units_per_split ? (n_pre + p.units_per_split - 1) / p.units_per_split : 1;
+        n_used = n_pre > per ? (n_pre + per - 1) / per : 1;
         if (split >= n_used) return;
         if (split == n_used - 1) u1 = n_units;
     }
@@ -436,7 +547,7 @@ __global__ __launch_bounds__(NW4 * 64, NR == 1 ? 4 : 2) void kv4_ways_kernel(Kv4
                 uint16_t *orow = p.out + ((int64_t)b * nq + (int64_t)(row / grp) * nq + h * grp + row % grp) * D;
                 *reinterpret_cast<bf16x4 *>(orow + ch * 4) = __builtin_convertvector(acc * (1.f / L), bf16x4);
             } else {
-                const int64_t prow = (((int64_t)b * p.n_split + split) * nkv + h) * rows + row;
+                const int64_t prow = ((int64_t)range * nkv + h) * rows + row;
                 *reinterpret_cast<f32x4 *>(p.o_part + prow * D + ch * 4) = acc;
                 if (ch == 0) p.ml_part[prow] = float2{M, L};
             }
@@ -758,21 +869,11 @@ __global__ __launch_bounds__(THREADS) void kv4_rows_kernel(Kv4Params p) {
 // sum of l_s.  d/4 threads of four dimensions for a (KV head, row) of request
 // blockIdx.y, and SG such groups over the splits of one row: with many splits their
 // partials are all in flight at once (61 splits of four rows: 9.4 us with SG = 1).
-template <int D, bool DECODE, int SG>
-__global__ __launch_bounds__(256) void kv4_merge_kernel(Kv4Params p) {
+template <int D, int SG>
+__device__ __forceinline__ void merge_rows(const Kv4Params &p, int b, int range0, int n_split, int last) {
     constexpr int TPR = D / 4, RPB = 256 / (TPR * SG), GS = 8;
-    const int b = DECODE ? (int)blockIdx.y : 0;
     const int sg = (int)threadIdx.x / TPR % SG, c4 = (int)threadIdx.x % TPR, in = (int)threadIdx.x / (TPR * SG);
     const int64_t gr = (int64_t)blockIdx.x * RPB + in;
-    int n_split = p.n_split;
-    if (DECODE) {
-        int Tp = p.num_tokens[b];
-        if (Tp < 0) return;
-        if (Tp > p.max_tokens) Tp = p.max_tokens;
-        const int n_pre = ((Tp + PAGE - 1) / PAGE + 1) / 2;
-        n_split = n_pre > p.units_per_split ? (n_pre + p.units_per_split - 1) / p.units_per_split : 1;
-        if (n_split == 1) return;                         // written by the attention itself
-    }
     float M = -__builtin_inff(), L = 0.f;
     f32x4 acc = {0.f, 0.f, 0.f, 0.f};
     const bool ok = gr < (int64_t)p.nkv * p.rows;
@@ -780,14 +881,15 @@ __global__ __launch_bounds__(256) void kv4_merge_kernel(Kv4Params p) {
     const int64_t row = ok ? gr - (int64_t)h * p.rows : 0;
     if (ok) {
         const int64_t step = (int64_t)p.nkv * p.rows;
-        const int64_t prow0 = ((int64_t)b * p.n_split * p.nkv + h) * p.rows + row;
+        const int64_t prow0 = (int64_t)h * p.rows + row;
         for (int s0 = sg; s0 < n_split; s0 += SG * GS) {
             float2 ml[GS];
             f32x4 o[GS];
 #pragma unroll
             for (int i = 0; i < GS; ++i) {
                 if (s0 + i * SG < n_split) {
-                    const int64_t prow = prow0 + (int64_t)(s0 + i * SG) * step;
+                    const int x = s0 + i * SG;
+                    const int64_t prow = prow0 + (int64_t)(x == n_split - 1 ? last : range0 + x) * step;
                     ml[i] = p.ml_part[prow];
                     o[i] = *reinterpret_cast<const f32x4 *>(p.o_part + prow * D + c4 * 4);
                 }
@@ -837,6 +939,27 @@ __global__ __launch_bounds__(256) void kv4_merge_kernel(Kv4Params p) {
     if (!ok) return;
     uint16_t *orow = p.out + ((int64_t)b * p.nq + row / p.grp * p.nq + h * p.grp + row % p.grp) * D;
     *reinterpret_cast<bf16x4 *>(orow + c4 * 4) = __builtin_convertvector(acc * (1.f / L), bf16x4);
+}
+
+template <int D, bool DECODE>
+__global__ __launch_bounds__(256) void kv4_merge_kernel(Kv4Params p) {
+    int b = 0, n_split = p.n_split, first = 0, last = n_split - 1;
+    if (DECODE) {
+        b = (int)blockIdx.y;
+        if (p.ranges) {
+            const int lane = (int)threadIdx.x & 63;
+            n_split = p.batch <= 64 ? RangeList<1>(p, lane).of_request(b, first, last)
+                                    : RangeList<2>(p, lane).of_request(b, first, last);
+        } else {
+            const int t = tokens_of(p, b), n = t < 0 ? 0 : units_of(t);
+            n_split = (n + p.units_per_split - 1) / p.units_per_split;
+            first = b * p.n_split;
+            last = first + n_split - 1;
+        }
+        if (n_split < 2) return;                          // written by the attention itself, or empty
+    }
+    if (n_split > 8) merge_rows<D, 8>(p, b, first, n_split, last);
+    else merge_rows<D, 1>(p, b, first, n_split, last);
 }
 
 // ---------------------------------------------------------------------------
@@ -957,13 +1080,21 @@ int plan_kv4_attention(const oc_layout &l, int64_t Tp, int64_t Ts, Kv4Plan *pl) 
     return OC_OK;
 }
 
-// Decode: the prefix units of each (request, KV head) in ranges of one length for all
-// requests, as many as its length has.  If all were as long as they may be, every CU
-// would get a workgroup, and requests much longer than the others are cut into ranges
-// of at most 160 units (some 30 us).  Up to 24 units are one range: a merge costs
-// 2.5 us, as much as two or three units per wavefront.  Many more ranges cost as
-// well: a workgroup that finds its request shorter takes 2 ns of the whole card (32
-// requests of up to 28560 tokens: 61 us in ranges of 96, 86 in ranges of 16).
+// Decode: the prefix units of each (request, KV head) in ranges that are work for one
+// workgroup.  Where lengths that differ can leave CUs idle, the kernels make the list
+// of ranges from the lengths (RangeList): one range to a CU if all were whole.  Against
+// ranges of one length chosen here for requests of max_tokens: 12 requests of 0 to
+// 19248 tokens 41 -> 15.8 us, 50 of up to 32K 52.7 -> 39.3, 53 of up to 32664 with 64
+// query heads 64 -> 56; requests of equal length within 4 % either way.  More ranges
+// were slower (256 / 512 / 768 of them: 43 / 46 / 44 us for 45 requests, 52 / 55 / 55 for
+// eight of 32000 tokens).
+//
+// Where every CU has a request anyway and none takes more than 160 units (some 30 us), a
+// list and a merge only cost (64 requests of up to 3000 tokens 18 us, 21 with them), as
+// they do past 128 requests.  Those, and single requests, get ranges of one length: as
+// many as would fill the CUs if all were as long as they may be, and of at most 160
+// units.  Up to 24 units are one range: a merge costs 2.5 us, as much as two or three
+// units per wavefront.
 int plan_kv4_decode(const oc_layout &l, int64_t batch, int64_t max_tokens, Kv4Plan *pl) {
     const int rc = attention_layout(l);
     if (rc) return rc;
@@ -983,17 +1114,30 @@ int plan_kv4_decode(const oc_layout &l, int64_t batch, int64_t max_tokens, Kv4Pl
     p.m_tiles = (int)((p.rows + p.row_tile - 1) / p.row_tile);
     p.n_units = (int)(((max_tokens + PAGE - 1) / PAGE + 1) / 2);
     const int64_t pairs = batch * p.nkv;
-    if (pairs > OC_MAX_GRID_ITEMS / THREADS) return fail(OC_ERANGE, "attention grid of more than 2^32 work-items");
     if (p.m_tiles > 65535) return fail(OC_ERANGE, "more than 2^20 query heads to a KV head");
-    const int64_t fill = std::max<int64_t>(1, 256 / (pairs * p.m_tiles));
-    int64_t ns = 1;
-    if (p.n_units > 3 * NW4) ns = (std::max<int64_t>(fill, (p.n_units + 159) / 160) + fill - 1) / fill * fill;
-    ns = std::min(ns, std::max<int64_t>(1, OC_MAX_GRID_ITEMS / THREADS / pairs));
-    const int64_t per = std::max<int64_t>(1, (p.n_units + ns - 1) / ns);
-    p.units_per_split = (int)((per + NW4 - 1) / NW4 * NW4);
-    p.n_split = std::max(1, (p.n_units + p.units_per_split - 1) / p.units_per_split);
+    const int64_t most = OC_MAX_GRID_ITEMS / THREADS / p.nkv;       // ranges a grid can have
+    const int64_t fill = 256 / (pairs * p.m_tiles);                // ranges of each pair that fill the CUs
+    int64_t n_ranges = batch;
+    p.n_split = 1;
+    p.units_per_split = std::max(3 * NW4, (p.n_units + NW4 - 1) / NW4 * NW4);
+    if (batch > 1 && batch <= 128 && batch * p.n_units < 1 << 24 && p.n_units > (fill ? 3 * NW4 : 160)) {
+        p.ranges = (int)std::max<int64_t>(1, 256 / ((int64_t)p.nkv * p.m_tiles));
+        p.units_per_split = NW4;                                  // at least
+        p.n_split = (p.n_units + NW4 - 1) / NW4;                  // at most, of one request
+        n_ranges = std::min(p.ranges + batch, batch * p.n_split);
+    } else if (p.n_units > 3 * NW4) {
+        const int64_t at_once = std::max<int64_t>(1, fill);
+        int64_t ns = (std::max<int64_t>(at_once, (p.n_units + 159) / 160) + at_once - 1) / at_once * at_once;
+        ns = std::min(ns, std::max<int64_t>(1, most / batch));
+        const int64_t per = (p.n_units + ns - 1) / ns;
+        p.units_per_split = (int)((per + NW4 - 1) / NW4 * NW4);
+        p.n_split = (p.n_units + p.units_per_split - 1) / p.units_per_split;
+        n_ranges = batch * p.n_split;
+    }
+    if (n_ranges > most) return fail(OC_ERANGE, "attention grid of more than 2^32 work-items");
+    p.n_ranges = (int32_t)n_ranges;
     if (pairs * p.rows * (p.d / 4) * 8 > OC_MAX_GRID_ITEMS) return fail(OC_ERANGE, "merge grid exceeds 2^32 work-items");
-    const int64_t rows = batch * p.n_split * p.nkv * p.rows;
+    const int64_t rows = n_ranges * p.nkv * p.rows;
     p.off_ml = p.n_split > 1 ? up256((size_t)rows * p.d * 4) : 0;
     p.total = p.n_split > 1 ? p.off_ml + up256((size_t)rows * 8) : 256;
     *pl = p;
@@ -1030,6 +1174,8 @@ static Kv4Params make_params(const Kv4Plan &pl, const Kv4AttnArgs &a) {
     p.units_per_split = pl.units_per_split;
     p.max_tokens = a.max_tokens;
     p.batch = pl.batch;
+    p.ranges = pl.ranges;
+    p.per_range = pl.ranges ? 1.f / (float)pl.ranges : 0.f;
     p.scale_log2 = (float)(1.4426950408889634 / sqrt((double)D));
     return p;
 }
@@ -1040,9 +1186,9 @@ static void launch_merge(const Kv4Params &p, unsigned requests, hipStream_t s) {
     constexpr int RPB = 256 / (D / 4);
     const int64_t n = (int64_t)p.nkv * p.rows;
     if (p.n_split > 8)
-        hipLaunchKernelGGL((kv4_merge_kernel<D, DECODE, 8>), dim3((unsigned)((n * 8 + RPB - 1) / RPB), requests), dim3(256), 0, s, p);
+        hipLaunchKernelGGL((kv4_merge_kernel<D, DECODE>), dim3((unsigned)((n * 8 + RPB - 1) / RPB), requests), dim3(256), 0, s, p);
     else
-        hipLaunchKernelGGL((kv4_merge_kernel<D, DECODE, 1>), dim3((unsigned)((n + RPB - 1) / RPB), requests), dim3(256), 0, s, p);
+        hipLaunchKernelGGL((kv4_merge_kernel<D, DECODE>), dim3((unsigned)((n + RPB - 1) / RPB), requests), dim3(256), 0, s, p);
 }
 
 template <int D>
@@ -1064,7 +1210,7 @@ static hipError_t launch_ways4(const Kv4Plan &pl, const Kv4AttnArgs &a, hipStrea
     static_assert(NW4 * 64 == THREADS, "the grid's limit is shared");
     const hipError_t e = allow_dynamic_lds<&kv4_ways_kernel<D, NR, PF, DECODE>>(LDS);
     if (e != hipSuccess) return e;
-    const dim3 grid = DECODE ? dim3((unsigned)(p.n_groups * pl.batch), (unsigned)pl.m_tiles) : dim3((unsigned)(p.n_groups * pl.m_tiles));
+    const dim3 grid = DECODE ? dim3((unsigned)(pl.n_ranges * pl.nkv), (unsigned)pl.m_tiles) : dim3((unsigned)(p.n_groups * pl.m_tiles));
     hipLaunchKernelGGL((kv4_ways_kernel<D, NR, PF, DECODE>), grid, dim3(NW4 * 64), LDS, s, p);
     launch_merge<D, DECODE>(p, DECODE ? (unsigned)pl.batch : 1u, s);
     return hipGetLastError();

@@ -384,6 +384,25 @@ def test_decode(nq, nkv, d, lengths):
     b.check(b.run())
 
 
+# (n_q, n_kv, d, lengths) that make a list of ranges: a lane to a request and two, equal and
+# very unequal lengths, whole ranges only, no tokens at all, empty places first and last
+def _lists():
+    rng = np.random.default_rng(21)
+    some = lambda n, most: (np.exp(rng.uniform(0, np.log(most), n)).astype(int) - 1).tolist()  # noqa: E731
+    return [
+        (8, 1, 64, [9000, 3, 0, -1, 1, 2500, 2500]), (4, 1, 128, [2048] * 3), (16, 8, 64, [1024] * 4), (2, 2, 64, [0, 0, 0]),
+        (2, 2, 64, [-1, -1]), (4, 4, 64, [-1, 1000, -1, -1]), (34, 1, 64, [1000, 30, 2000]), (8, 8, 64, [40] + some(20, 7000)),
+        (4, 1, 64, some(64, 3000)), (4, 1, 64, some(65, 3000)), (2, 1, 64, [-1] + some(126, 2000) + [-1]),
+        (6, 3, 64, [1900] * 80), (4, 1, 64, [0] * 64 + [6000]), (4, 1, 64, [6000] + [-1] * 127),
+    ]
+
+
+@pytest.mark.parametrize("nq,nkv,d,lengths", _lists())
+def test_decode_by_list(nq, nkv, d, lengths):
+    b = Batch(nq, nkv, d, lengths, room=800)
+    b.check(b.run())
+
+
 def test_decode_long_and_short_together():
     b = Batch(8, 1, 128, [20000, 3, 9000, 0, 500, -1, 31])
     first = b.run()

@@ -124,7 +124,49 @@ def test_plans_cover_rows_and_keys():
         assert m_tiles * tile >= nq // nkv and units == -(-(-(-tp // 16)) // 2) and per % 8 == 0
         assert splits * per >= units and (splits == 1 or (splits - 1) * per < units)
         need = oc.oc_kv4_decode_workspace_bytes(oc.Layout(1, nq, nkv, d, 16, 16, 8), batch, tp)
-        assert need >= (splits * batch * nq * (d + 2) * 4 if splits > 1 else 256)
+        assert need >= (decode_ranges(nq, nkv, d, batch, tp)[1] * nq * (d + 2) * 4 if splits > 1 else 256)
+
+
+def decode_ranges(nq, nkv, d, batch, most):
+    """Ranges wanted (0: no list), ranges at most."""
+    lay, out = L.c_layout(1, nq, nkv, d, 16, 16, 1 << 40), (c_int64 * 2)()
+    assert oc.lib().oc_internal_kv4_ranges(ctypes.byref(lay), c_int64(batch), c_int64(most), out) == 0
+    return tuple(out)
+
+
+def test_the_ranges_of_a_decode_have_their_workgroups():
+    """Whatever the lengths: as many ranges as were planned for at most, every unit in one, and counts that the
+    list's fields hold."""
+    rng = np.random.default_rng(4)
+    lists = 0
+    for _ in range(3000):
+        nkv = int(rng.integers(1, 17))
+        nq, d, batch = nkv * int(rng.integers(1, 20)), int(rng.choice([64, 128])), int(np.exp(rng.uniform(0, 6)))
+        most = int(np.exp(rng.uniform(0, 11)))
+        wanted, at_most = decode_ranges(nq, nkv, d, batch, most)
+        _, m_tiles, _, splits, per = plan(nq, nkv, d, most, 1, batch)
+        kind = rng.integers(4)
+        lengths = (np.full(batch, most) if kind == 0 else np.exp(rng.uniform(0, np.log(most + 1), batch)).astype(int) - 1
+                   if kind == 1 else np.where(rng.random(batch) < 0.1, most, 0) if kind == 2 else rng.integers(-1, most + 1, batch))
+        units = -(-(-(-np.maximum(lengths, 0) // 16)) // 2)
+        if wanted:
+            lists += 1
+            # the kernels' own arithmetic, in 32 bits
+            per = max(per, (int(np.float32(units.sum()) * (np.float32(1) / np.float32(wanted))) + 8) // 8 * 8)
+            assert units.sum() < 1 << 24 and per * wanted >= units.sum() and batch <= 128
+            assert (units // per).sum() <= wanted < 1024 and wanted * nkv * m_tiles <= max(256, nkv * m_tiles)
+        else:
+            assert at_most == batch * splits
+        assert np.where(lengths < 0, 0, np.maximum(1, -(-units // per))).sum() <= at_most
+    assert lists > 300
+
+
+def test_which_decodes_make_a_list():
+    for args, want in (((32, 8, 128, 1, 30000), 0), ((32, 8, 128, 2, 768), 0), ((32, 8, 128, 2, 769), 32),
+                       ((32, 8, 128, 32, 5120), 32), ((32, 8, 128, 33, 5120), 0), ((32, 8, 128, 33, 5121), 32),
+                       ((32, 8, 128, 128, 30000), 32), ((32, 8, 128, 129, 30000), 0), ((64, 1, 128, 2, 4000), 128),
+                       ((512, 512, 64, 4, 30000), 1), ((8, 1, 128, 128, 1 << 23), 0)):
+        assert decode_ranges(*args)[0] == want, args
 
 
 # ---- refusals ---------------------------------------------------------------
