@@ -8,6 +8,11 @@
 // instruction reads whole rows of the payload (d = 128: four rows of 256 bytes) and
 // the codes of the page go out as one contiguous stretch.  The four lanes of a quad
 // hold one block and find its largest magnitude among themselves.
+//
+// Bound by memory: a layer of 65536 tokens of 8 heads of 128 is stored in 68 us (340
+// MB, 5.0 TB/s) and 66048 of them read back in 50 (342 MB; the codes, just written, are
+// partly in the last cache).  A copy of 1 GiB moves 5.1 TB/s.  The least calls (256
+// tokens) take 3.2 us, a launch.
 #include "kv4.hpp"
 
 namespace oc {

@@ -41,6 +41,16 @@ struct Kv4Params {
 // per lane.  The P of two pages is then the second operand of O^T += V^T P as it
 // stands, its contraction index 8g + i being key 4g + i%4 of page i/4; V is decoded
 // into LDS and read back transposed, four keys of one page per read.
+//
+// What bounds it, and measured: decode by its codes and scales from memory (eight
+// requests of 32K tokens at 64/8/128: 272 MB in 48.5 us, 5.6 TB/s; 30 of 0 to 28560 at
+// 32/8/128: 210 MB in 42.6, 4.9 TB/s; matrix units 10 % busy, vector units 30 %).  One new
+// token over 32763: 35.7 MB in 9.1 us and a merge of 2.6.  At 128 new tokens over
+// 4096 two workgroups of each CU do a chain of four dependent rounds per wavefront (load,
+// product, softmax, LDS, product): 22 us in all, where its products alone are 7 at the
+// rate of a large one.  Sixteen wavefronts to a workgroup, two or three units ahead, and
+// the next unit's scores before this one's softmax did not shorten it; 64-row tiles with
+// Q in LDS gained at one shape of the 75 below (512 tokens over 1024).
 // ---------------------------------------------------------------------------
 
 // XOR on the 16-byte column of V row r (key in its page).  The columns of eight
@@ -567,6 +577,11 @@ __global__ __launch_bounds__(NW4 * 64, NR == 1 ? 4 : 2) void kv4_ways_kernel(Kv4
 // page is copied straight to LDS.  Decoding costs 16 conversions per lane and block
 // beside some 130 vector operations of the softmax, and the codes a quarter of the
 // bytes, so the matrix phases bound this kernel as they do the bfloat16 one.
+//
+// 512 tokens over 65536 at 32/8/128: 5.52e11 operations in 507 us with its merge, 1.09
+// PFLOP/s, where a bfloat16 product of 8192^3 reaches 1.23; matrix units 45 % busy, vector
+// units 43 %.  A product with the codes as they are (scaled 4-bit by 8-bit, Q in two
+// 8-bit terms) takes as many matrix cycles and a longer start.
 // ---------------------------------------------------------------------------
 template <int D>
 __global__ __launch_bounds__(THREADS) void kv4_rows_kernel(Kv4Params p) {
@@ -866,11 +881,13 @@ __global__ __launch_bounds__(THREADS) void kv4_rows_kernel(Kv4Params p) {
 }
 
 // Merge the splits of each row: weights 2^(m_s - M), normalised by the matching
-// sum of l_s.  d/4 threads of four dimensions for a (KV head, row) of request
-// blockIdx.y, and SG such groups over the splits of one row: with many splits their
-// partials are all in flight at once (61 splits of four rows: 9.4 us with SG = 1).
+// sum of l_s.  d/4 threads of four dimensions for a (KV head, row), and SG such
+// groups over the splits of one row: with many splits their partials are all in
+// flight at once (61 splits of four rows: 9.4 us with SG = 1, 3.9 with 8).  Bound by
+// its bytes where there are many rows: the two splits of 512 tokens of 32 heads, 34 MB,
+// in 8.3 us (4.0 TB/s).  Split s is partial first + s, the last one partial `last`.
 template <int D, int SG>
-__device__ __forceinline__ void merge_rows(const Kv4Params &p, int b, int range0, int n_split, int last) {
+__device__ __forceinline__ void merge_rows(const Kv4Params &p, int b, int first, int n_split, int last) {
     constexpr int TPR = D / 4, RPB = 256 / (TPR * SG), GS = 8;
     const int sg = (int)threadIdx.x / TPR % SG, c4 = (int)threadIdx.x % TPR, in = (int)threadIdx.x / (TPR * SG);
     const int64_t gr = (int64_t)blockIdx.x * RPB + in;
@@ -889,7 +906,7 @@ __device__ __forceinline__ void merge_rows(const Kv4Params &p, int b, int range0
             for (int i = 0; i < GS; ++i) {
                 if (s0 + i * SG < n_split) {
                     const int x = s0 + i * SG;
-                    const int64_t prow = prow0 + (int64_t)(x == n_split - 1 ? last : range0 + x) * step;
+                    const int64_t prow = prow0 + (int64_t)(x == n_split - 1 ? last : first + x) * step;
                     ml[i] = p.ml_part[prow];
                     o[i] = *reinterpret_cast<const f32x4 *>(p.o_part + prow * D + c4 * 4);
                 }
@@ -941,23 +958,27 @@ __device__ __forceinline__ void merge_rows(const Kv4Params &p, int b, int range0
     *reinterpret_cast<bf16x4 *>(orow + c4 * 4) = __builtin_convertvector(acc * (1.f / L), bf16x4);
 }
 
-template <int D, bool DECODE>
+template <int D, int SG>
 __global__ __launch_bounds__(256) void kv4_merge_kernel(Kv4Params p) {
-    int b = 0, n_split = p.n_split, first = 0, last = n_split - 1;
-    if (DECODE) {
-        b = (int)blockIdx.y;
-        if (p.ranges) {
-            const int lane = (int)threadIdx.x & 63;
-            n_split = p.batch <= 64 ? RangeList<1>(p, lane).of_request(b, first, last)
-                                    : RangeList<2>(p, lane).of_request(b, first, last);
-        } else {
-            const int t = tokens_of(p, b), n = t < 0 ? 0 : units_of(t);
-            n_split = (n + p.units_per_split - 1) / p.units_per_split;
-            first = b * p.n_split;
-            last = first + n_split - 1;
-        }
-        if (n_split < 2) return;                          // written by the attention itself, or empty
+    merge_rows<D, SG>(p, 0, 0, p.n_split, p.n_split - 1);
+}
+
+// The same for request blockIdx.y of a decode, whose splits only the device knows.
+template <int D>
+__global__ __launch_bounds__(256) void kv4_decode_merge_kernel(Kv4Params p) {
+    const int b = (int)blockIdx.y;
+    int n_split, first, last;
+    if (p.ranges) {
+        const int lane = (int)threadIdx.x & 63;
+        n_split = p.batch <= 64 ? RangeList<1>(p, lane).of_request(b, first, last)
+                                : RangeList<2>(p, lane).of_request(b, first, last);
+    } else {
+        const int t = tokens_of(p, b), n = t < 0 ? 0 : units_of(t);
+        n_split = (n + p.units_per_split - 1) / p.units_per_split;
+        first = b * p.n_split;
+        last = first + n_split - 1;
     }
+    if (n_split < 2) return;                              // written by the attention itself, or empty
     if (n_split > 8) merge_rows<D, 8>(p, b, first, n_split, last);
     else merge_rows<D, 1>(p, b, first, n_split, last);
 }
@@ -1180,15 +1201,16 @@ static Kv4Params make_params(const Kv4Plan &pl, const Kv4AttnArgs &a) {
     return p;
 }
 
-template <int D, bool DECODE>
+// `requests`: 0 for one request's suffix
+template <int D>
 static void launch_merge(const Kv4Params &p, unsigned requests, hipStream_t s) {
     if (p.n_split < 2) return;
     constexpr int RPB = 256 / (D / 4);
-    const int64_t n = (int64_t)p.nkv * p.rows;
-    if (p.n_split > 8)
-        hipLaunchKernelGGL((kv4_merge_kernel<D, DECODE>), dim3((unsigned)((n * 8 + RPB - 1) / RPB), requests), dim3(256), 0, s, p);
-    else
-        hipLaunchKernelGGL((kv4_merge_kernel<D, DECODE>), dim3((unsigned)((n + RPB - 1) / RPB), requests), dim3(256), 0, s, p);
+    const int64_t n = (int64_t)p.nkv * p.rows * (p.n_split > 8 ? 8 : 1);
+    const dim3 grid((unsigned)((n + RPB - 1) / RPB), std::max(1u, requests));
+    if (requests) hipLaunchKernelGGL(kv4_decode_merge_kernel<D>, grid, dim3(256), 0, s, p);
+    else if (p.n_split > 8) hipLaunchKernelGGL((kv4_merge_kernel<D, 8>), grid, dim3(256), 0, s, p);
+    else hipLaunchKernelGGL((kv4_merge_kernel<D, 1>), grid, dim3(256), 0, s, p);
 }
 
 template <int D>
@@ -1198,7 +1220,7 @@ static hipError_t launch_rows(const Kv4Plan &pl, const Kv4AttnArgs &a, hipStream
     if (e != hipSuccess) return e;
     const Kv4Params p = make_params<D>(pl, a);
     hipLaunchKernelGGL(kv4_rows_kernel<D>, dim3((unsigned)rows_grid(pl)), dim3(THREADS), LDS, s, p);
-    launch_merge<D, false>(p, 1, s);
+    launch_merge<D>(p, 0, s);
     return hipGetLastError();
 }
 
@@ -1212,7 +1234,7 @@ static hipError_t launch_ways4(const Kv4Plan &pl, const Kv4AttnArgs &a, hipStrea
     if (e != hipSuccess) return e;
     const dim3 grid = DECODE ? dim3((unsigned)(pl.n_ranges * pl.nkv), (unsigned)pl.m_tiles) : dim3((unsigned)(p.n_groups * pl.m_tiles));
     hipLaunchKernelGGL((kv4_ways_kernel<D, NR, PF, DECODE>), grid, dim3(NW4 * 64), LDS, s, p);
-    launch_merge<D, DECODE>(p, DECODE ? (unsigned)pl.batch : 1u, s);
+    launch_merge<D>(p, DECODE ? (unsigned)pl.batch : 0u, s);
     return hipGetLastError();
 }
 
