@@ -344,7 +344,9 @@ size_t oc_kv4_decode_workspace_bytes(const oc_layout *layout, int64_t batch, int
  * be no other table's (oc_kv_pages_fork sees to that).  An id outside [0, P), as
  * a fork or take without enough pages leaves it, touches nothing outside the pool:
  * the token is not appended, or page 0 is read in its place (and that row means
- * nothing).  batch == 0 is not an error; batch <= 65535.  workspace: device, at least
+ * nothing).  The keys are divided by the lengths of the whole batch, and a row's
+ * last bits depend on the division; for the same lengths they are always the same.
+ * batch == 0 is not an error; batch <= 65535.  workspace: device, at least
  * oc_kv4_decode_workspace_bytes(), 256-byte aligned, as for
  * oc_kv4_suffix_prefill_layer.  Asynchronous on `stream`. */
 int oc_kv4_decode_layer(const void *q, const void *k_new, const void *v_new, int64_t batch, oc_kv_pool *kv_pool,
