@@ -4,13 +4,13 @@
 // stream order: no call waits for the host.
 //
 // Two kinds of kernel.  A plan (which pages are free, which move where) is one
-// workgroup's scan over the counts, 16 pages to a thread: 4 bytes a page.  The copies
+// workgroup's scan over the counts, one page or 16 to a thread: 4 bytes a page.  The copies
 // are 16-byte pieces with remapped pages, bound by memory.
 //
 // Measured, in a pool of 512 pages of 32 layers (2 MB a page): 160 pages move in 138 us
-// (671 MB, 4.9 TB/s; a copy of 1 GiB moves 5.1) after a plan of 6.8; sixteen copies of
-// one page take 9.8 us (33.6 MB written, 3.4 TB/s: the start and the end of a launch are
-// as long as what lies between) after a take of 3.5.
+// (671 MB, 4.9 TB/s; a copy of 1 GiB moves 5.1) after a plan of 4.3; sixteen copies of
+// one page take 10 us (33.6 MB written, 3.4 TB/s: the start and the end of a launch are
+// as long as what lies between) after a take of 2.8.
 #include <algorithm>
 
 #include "common.hpp"
@@ -21,7 +21,7 @@ typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 
 constexpr int kCopyThreads = 256;
 constexpr int kSegment = kCopyThreads * 8 * 16;       // bytes of one workgroup's piece of a page
-constexpr int kPlanThreads = 1024, kPlanPages = 16;   // pages of a plan's thread and step
+constexpr int kPlanThreads = 1024;
 
 // Copy `bytes` (a multiple of 16, at most kSegment) with one workgroup: eight
 // loads of a thread in flight.  What is written is not read again soon, so it
@@ -88,38 +88,45 @@ __device__ inline uint32_t block_scan(uint32_t x, uint32_t *total, uint32_t *lds
     return before + s - x;
 }
 
-// Which of this thread's kPlanPages pages from `first` on are held (one bit each).
+// Which of this thread's N pages from `first` on are held (one bit each).  N is 1 where
+// that covers the pool, so that no thread goes through several pages one after the
+// other (512 pages: a take 3.5 -> 2.8 us, a plan 6.8 -> 4.3), else 16, four loads at once.
+template <int N>
 __device__ inline uint32_t held_pages(const int32_t *counts, int64_t first, int32_t num_pages) {
     typedef int32_t i32x4 __attribute__((ext_vector_type(4), aligned(4)));
     uint32_t held = 0;
-    if (first + kPlanPages <= num_pages) {
-        i32x4 c[kPlanPages / 4];
+    if constexpr (N % 4 == 0) {
+        if (first + N <= num_pages) {
+            i32x4 c[N / 4];
 #pragma unroll
-        for (int i = 0; i < kPlanPages / 4; ++i) c[i] = *reinterpret_cast<const i32x4 *>(counts + first + i * 4);
+            for (int i = 0; i < N / 4; ++i) c[i] = *reinterpret_cast<const i32x4 *>(counts + first + i * 4);
 #pragma unroll
-        for (int i = 0; i < kPlanPages; ++i) held |= (uint32_t)(c[i / 4][i % 4] > 0) << i;
-        return held;
+            for (int i = 0; i < N; ++i) held |= (uint32_t)(c[i / 4][i % 4] > 0) << i;
+            return held;
+        }
     }
 #pragma unroll
-    for (int i = 0; i < kPlanPages; ++i)
+    for (int i = 0; i < N; ++i)
         if (first + i < num_pages) held |= (uint32_t)(counts[first + i] > 0) << i;
     return held;
 }
+template <int N>
 __device__ inline uint32_t pages_below(int64_t first, int64_t limit) {
     const int64_t n = limit - first;
-    return n <= 0 ? 0u : n >= kPlanPages ? (1u << kPlanPages) - 1 : (1u << n) - 1;
+    return n <= 0 ? 0u : n >= N ? (1u << N) - 1 : (1u << n) - 1;
 }
 
 // The n lowest free pages, in order, to out[i * stride], with a count of 1;
 // *status 0.  With fewer than n free: -1 to all of them, *status OC_ENOMEM, the
 // counts as they were.
+template <int N>
 __global__ __launch_bounds__(kPlanThreads) void pages_take_kernel(PagesArgs a, int32_t n, int32_t *out, int64_t stride) {
     __shared__ uint32_t sums[kPlanThreads / 64];
-    constexpr int64_t STEP = (int64_t)kPlanThreads * kPlanPages;
+    constexpr int64_t STEP = (int64_t)kPlanThreads * N;
     int64_t found = 0;
     for (int64_t p0 = 0; p0 < a.num_pages && found < n; p0 += STEP) {
-        const int64_t first = p0 + (int64_t)threadIdx.x * kPlanPages;
-        uint32_t free = ~held_pages(a.counts, first, a.num_pages) & pages_below(first, a.num_pages), total;
+        const int64_t first = p0 + (int64_t)threadIdx.x * N;
+        uint32_t free = ~held_pages<N>(a.counts, first, a.num_pages) & pages_below<N>(first, a.num_pages), total;
         int64_t at = found + block_scan((uint32_t)__popc(free), &total, sums);
         for (; free && at < n; free &= free - 1, ++at) out[at * stride] = (int32_t)(first + __ffs(free) - 1);
         found += total;
@@ -176,35 +183,36 @@ __device__ __host__ inline int64_t ws_map(int64_t P) { return 16 + 2 * (P / 2 + 
 // ones before it, in order: as many of each, and no page is read and written.  With
 // b(p) held pages before page p, a free page p in front is the (p - b(p))-th target
 // and a held one behind the (b(p) - b(live))-th source, so one scan gives both.
+template <int N>
 __global__ __launch_bounds__(kPlanThreads) void pages_plan_kernel(PagesArgs a, int32_t *ws, int32_t *num_live) {
     constexpr int NEAR = 2048;                        // moves whose ids stay in LDS too
     __shared__ uint32_t sums[kPlanThreads / 64];
     __shared__ int32_t near_src[NEAR], near_dst[NEAR];
     __shared__ int64_t before_live;
-    constexpr int64_t STEP = (int64_t)kPlanThreads * kPlanPages;
+    constexpr int64_t STEP = (int64_t)kPlanThreads * N;
     const int64_t P = a.num_pages;
     int32_t *const src = ws + ws_src(P), *const dst = ws + ws_dst(P), *const map = ws + ws_map(P);
     uint32_t held = 0, below = 0, total = 0;          // this thread's pages, those held before them, and in the step
     int64_t live = 0;
     for (int64_t p0 = 0; p0 < P; p0 += STEP) {
-        held = held_pages(a.counts, p0 + (int64_t)threadIdx.x * kPlanPages, a.num_pages);
+        held = held_pages<N>(a.counts, p0 + (int64_t)threadIdx.x * N, a.num_pages);
         below = block_scan((uint32_t)__popc(held), &total, sums);
         live += total;
     }
     int64_t run = 0;
     for (int64_t p0 = 0; p0 < P; p0 += STEP) {
-        const int64_t first = p0 + (int64_t)threadIdx.x * kPlanPages;
+        const int64_t first = p0 + (int64_t)threadIdx.x * N;
         if (P > STEP) {                               // else the pass above has them
-            held = held_pages(a.counts, first, a.num_pages);
+            held = held_pages<N>(a.counts, first, a.num_pages);
             below = block_scan((uint32_t)__popc(held), &total, sums);
         }
         const int64_t b = run + below;
         if (live >= p0 && live < p0 + STEP) {         // the step that has page `live`: no source came before it
-            if (live >= first && live < first + kPlanPages)
+            if (live >= first && live < first + N)
                 before_live = b + __popc(held & ((1u << (live - first)) - 1));
             __syncthreads();
         }
-        const uint32_t low = pages_below(first, live), here = pages_below(first, P);
+        const uint32_t low = pages_below<N>(first, live), here = pages_below<N>(first, P);
         // (the bounds hold unless another stream changes the counts meanwhile)
         for (uint32_t f = ~held & low; f; f &= f - 1) {
             const int i = __ffs(f) - 1;
@@ -222,7 +230,7 @@ __global__ __launch_bounds__(kPlanThreads) void pages_plan_kernel(PagesArgs a, i
                 if (m < NEAR) near_src[m] = (int32_t)(first + i);
             }
         }
-        for (int i = 0; i < kPlanPages && first + i < P; ++i) map[first + i] = (int32_t)(first + i);
+        for (int i = 0; i < N && first + i < P; ++i) map[first + i] = (int32_t)(first + i);
         run += total;
     }
     __syncthreads();
@@ -264,7 +272,10 @@ __global__ __launch_bounds__(kCopyThreads) void pages_move_kernel(PagesArgs a, i
 static unsigned copy_grid(int64_t items) { return (unsigned)std::max<int64_t>(1, std::min<int64_t>(items, 2048)); }
 
 hipError_t launch_pages_take(const PagesArgs &a, int32_t n, int32_t *out, int64_t stride, hipStream_t s) {
-    hipLaunchKernelGGL(pages_take_kernel, dim3(1), dim3(kPlanThreads), 0, s, a, n, out, stride);
+    if (a.num_pages <= kPlanThreads)
+        hipLaunchKernelGGL(pages_take_kernel<1>, dim3(1), dim3(kPlanThreads), 0, s, a, n, out, stride);
+    else
+        hipLaunchKernelGGL(pages_take_kernel<16>, dim3(1), dim3(kPlanThreads), 0, s, a, n, out, stride);
     return hipGetLastError();
 }
 
@@ -297,7 +308,10 @@ size_t pages_workspace_bytes(int64_t num_pages) { return (size_t)(ws_map(num_pag
 
 hipError_t launch_pages_compact(const PagesArgs &a, int32_t *tables, int32_t n_tables, int32_t entries, int64_t stride,
                                 int32_t *num_live, int32_t *ws, hipStream_t s) {
-    hipLaunchKernelGGL(pages_plan_kernel, dim3(1), dim3(kPlanThreads), 0, s, a, ws, num_live);
+    if (a.num_pages <= kPlanThreads)
+        hipLaunchKernelGGL(pages_plan_kernel<1>, dim3(1), dim3(kPlanThreads), 0, s, a, ws, num_live);
+    else
+        hipLaunchKernelGGL(pages_plan_kernel<16>, dim3(1), dim3(kPlanThreads), 0, s, a, ws, num_live);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
     // the moves are counted on the device: enough workgroups for as many as there can be
