@@ -279,7 +279,11 @@ int oc_rest_of_layer(const void *attn_out, int64_t tokens, const oc_layout *layo
  * These entry points take the layouts of the bfloat16 ones where head_dim is
  * a multiple of 32 (attention: 64 or 128, with a page_size of 16); their checks,
  * errors and streams are those of the entry points they are named after.
- * Positions are 32-bit: 2^31 tokens or more are OC_ERANGE.
+ * Positions are 32-bit: 2^31 tokens or more are OC_ERANGE.  A page id outside
+ * [0, P), as a fork or take without enough pages leaves it (oc_kv_pages_* below),
+ * touches nothing outside the pool in any of them: nothing is stored to or read
+ * back from such a page (its part of a payload stays as it was), and attention
+ * reads page 0 in its place, so that its rows mean nothing.
  * ------------------------------------------------------------------------- */
 
 /* Bytes of a 4-bit pool of this layout (0: the layout is not supported). */

@@ -17,6 +17,9 @@ int check_kv4_layout(const oc_layout &l) {
     return OC_OK;
 }
 
+// page ids are 32-bit: those of a larger pool are all within it
+static int32_t pages_of(const oc_layout &l) { return (int32_t)std::min<int64_t>(l.num_pages, INT32_MAX); }
+
 static Kv4Args kv4_args(const oc_kv_pool *pool, const oc_block_table *bt, int32_t layer, int64_t first, int64_t tokens) {
     const oc_layout &l = pool->layout;
     Kv4Args a{};
@@ -31,6 +34,7 @@ static Kv4Args kv4_args(const oc_kv_pool *pool, const oc_block_table *bt, int32_
     a.n_kv = l.num_kv_heads;
     a.d = l.head_dim;
     a.Ps = l.page_size;
+    a.num_pages = pages_of(l);
     return a;
 }
 
@@ -129,6 +133,7 @@ static Kv4AttnArgs attention_args(const void *q, const void *k_new, const void *
     a.pool_v = a.pool_k + l.num_pages * a.page_bytes;
     a.out = static_cast<uint16_t *>(out);
     a.ws = static_cast<unsigned char *>(workspace);
+    a.num_pages = pages_of(l);
     return a;
 }
 
@@ -197,7 +202,6 @@ static int decode(const void *q, const void *k_new, const void *v_new, int64_t b
     a.table_stride = tables->stride;
     a.num_tokens = num_tokens;
     a.max_tokens = (int32_t)max_tokens;
-    a.num_pages = (int32_t)std::min<int64_t>(l.num_pages, INT32_MAX);      // ids are 32-bit
     OC_HIP(launch_kv4_attention(p, a, static_cast<hipStream_t>(stream)));
     return OC_OK;
 }

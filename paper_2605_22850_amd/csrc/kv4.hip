@@ -28,7 +28,9 @@ __device__ inline int64_t payload_at(const Kv4Args &a, uint32_t T, int kv, int h
     return ((((int64_t)j * 2 + kv) * a.G + t) * a.n_kv + h) * a.d + c * 8;
 }
 
-// Which page, half and head this wavefront has; false past the last.
+// Which page, half and head this wavefront has; false past the last, and where the
+// table names no page of the pool (a fork or take that found none leaves -1, which the
+// host does not see).
 struct Unit {
     int kv, h;
     uint32_t q;              // page of the table
@@ -40,9 +42,11 @@ __device__ inline bool unit_of(const Kv4Args &a, Unit &u) {
     const uint32_t n = i / per_page, r = i - n * per_page;
     u.q = (uint32_t)a.first / (uint32_t)a.Ps + n;
     if ((int64_t)u.q * a.Ps >= a.end) return false;
+    const int32_t id = a.pages[u.q];
+    if ((uint32_t)id >= (uint32_t)a.num_pages) return false;
     u.kv = r >= (uint32_t)a.n_kv;
     u.h = (int)(r - (u.kv ? (uint32_t)a.n_kv : 0u));
-    u.page = (u.kv ? a.pool_v : a.pool_k) + (int64_t)a.pages[u.q] * a.page_bytes;
+    u.page = (u.kv ? a.pool_v : a.pool_k) + (int64_t)id * a.page_bytes;
     return true;
 }
 

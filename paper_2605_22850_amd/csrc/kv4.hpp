@@ -36,6 +36,7 @@ struct Kv4Args {
     int32_t code_bytes;           // of one page
     int32_t first, end;           // logical positions written or read
     int32_t G, n_kv, d, Ps;
+    int32_t num_pages;            // ids outside [0, num_pages) name no page: nothing of them is touched
     int32_t lg_g, lg_d8;          // -1: no power of two (filled by the launcher)
 };
 hipError_t launch_kv4_ingest(Kv4Args a, hipStream_t s);

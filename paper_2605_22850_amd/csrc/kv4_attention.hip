@@ -370,8 +370,8 @@ __global__ __launch_bounds__(NW4 * 64, NR == 1 ? 4 : 2) void kv4_ways_kernel(Kv4
         int pg = 2 * (u + (lane >> 1) * NW4) + (lane & 1);
         if (pg > n_pre_pages - 1) pg = n_pre_pages - 1;
         int32_t id = pages[pg];
-        // (a table of the decode form may hold what a fork or take left that found no page)
-        if (DECODE && (uint32_t)id >= (uint32_t)p.num_pages) id = 0;
+        // (the table may hold what a fork or take left that found no page)
+        if ((uint32_t)id >= (uint32_t)p.num_pages) id = 0;
         at = reinterpret_cast<uint64_t>(p.pool_k) + (uint64_t)((int64_t)id * page_bytes);
     };
     auto code_at = [&](int slot) { return head_codes + slot * (D / 2) + g * (D / 8); };
@@ -601,6 +601,7 @@ __global__ __launch_bounds__(THREADS) void kv4_rows_kernel(Kv4Params p) {
     const int rows = p.rows, Tp = p.Tp, Ts = p.Ts, n_pre_pages = (Tp + PAGE - 1) / PAGE;
     const float scale_log2 = p.scale_log2;
     const int64_t page_bytes = p.page_bytes;
+    const int num_pages = p.num_pages;
     const unsigned char *const pool = is_v ? p.pool_v : p.pool_k;
     const uint16_t *const dense = is_v ? p.v_new : p.k_new;
     const __attribute__((address_space(4))) int32_t *pages_c =
@@ -653,6 +654,9 @@ __global__ __launch_bounds__(THREADS) void kv4_rows_kernel(Kv4Params p) {
         Raw r{};
         const int v = page_of(j);
         if (v >= n_pre_pages) return r;
+        // (the table may hold what a fork or take left that found no page; checked here and
+        // not at the load, which is a block ahead and not waited for)
+        if ((uint32_t)pid >= (uint32_t)num_pages) pid = 0;
         // slots behind the last token repeat it: they are masked, and never read
         const int left = Tp - 1 - v * PAGE;
         const uint32_t slot = (uint32_t)(key < left ? key : left);
