@@ -78,8 +78,12 @@ typedef struct {
 /* Block table of one request: device int32 page ids.  Logical prefix token T
  * lives in page pages[T / page_size] at slot T % page_size.  num_tokens is the
  * cached prefix length; num_entries >= ceil(num_tokens / page_size).  Page ids
- * must be distinct and in [0, P); the kernels trust them (validate with
- * oc_block_table_check when the table is not trusted). */
+ * must be distinct and in [0, P); oc_block_table_check says whether those of a
+ * table in host memory are.  A device table may hold ids outside [0, P) where a
+ * fork or take found no page (oc_kv_pages_* below): no call touches anything
+ * outside the pool for them.  Nothing is stored to or copied from such a page
+ * (its part of a payload or object stays as it was), and attention reads some
+ * page of the pool in its place, so that its rows mean nothing. */
 typedef struct {
     const int32_t *pages;
     int64_t num_entries;
@@ -279,11 +283,8 @@ int oc_rest_of_layer(const void *attn_out, int64_t tokens, const oc_layout *layo
  * These entry points take the layouts of the bfloat16 ones where head_dim is
  * a multiple of 32 (attention: 64 or 128, with a page_size of 16); their checks,
  * errors and streams are those of the entry points they are named after.
- * Positions are 32-bit: 2^31 tokens or more are OC_ERANGE.  A page id outside
- * [0, P), as a fork or take without enough pages leaves it (oc_kv_pages_* below),
- * touches nothing outside the pool in any of them: nothing is stored to or read
- * back from such a page (its part of a payload stays as it was), and attention
- * reads page 0 in its place, so that its rows mean nothing.
+ * Positions are 32-bit: 2^31 tokens or more are OC_ERANGE.  For page ids outside
+ * [0, P) holds what oc_block_table says; attention reads page 0 in their place.
  * ------------------------------------------------------------------------- */
 
 /* Bytes of a 4-bit pool of this layout (0: the layout is not supported). */
@@ -365,7 +366,9 @@ int oc_kv4_decode_layer(const void *q, const void *k_new, const void *v_new, int
  * on the device in the order of `stream`; what only the device can find out, that
  * no page is left, goes to a device int32 `status` (OC_OK or OC_ENOMEM).
  * Calls that share page_counts must be ordered.  Page ids outside [0, P) in
- * device tables are left out.
+ * device tables are left out.  Calls queued behind a fork or take before the host
+ * has read `status` may meet the -1 that one without enough pages leaves: they are
+ * harmless (oc_block_table), and what they were to store has to be stored again.
  * ------------------------------------------------------------------------- */
 
 /* The n lowest free pages, ascending, to device pages_out[0..n), each with a

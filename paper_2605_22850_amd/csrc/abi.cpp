@@ -64,6 +64,7 @@ static IngestArgs ingest_args(const oc_kv_pool *pool, const oc_block_table *bt, 
     a.n_kv = l.num_kv_heads;
     a.d = l.head_dim;
     a.Ps = l.page_size;
+    a.num_pages = pages_of(l);
     return a;
 }
 
@@ -98,6 +99,7 @@ AppendArgs append_args(const oc_kv_pool *pool, const oc_block_table *bt, int32_t
     a.n_kv = l.num_kv_heads;
     a.d = l.head_dim;
     a.Ps = l.page_size;
+    a.num_pages = pages_of(l);
     return a;
 }
 
@@ -417,6 +419,7 @@ static int enqueue_attention(const AttnPlan &p, const void *q, const void *k_new
     a.pool_k = base + ((int64_t)layer * 2 + 0) * l.num_pages * block;
     a.pool_v = base + ((int64_t)layer * 2 + 1) * l.num_pages * block;
     a.pages = block_table->pages;
+    a.num_pages = pages_of(l);
     a.out = static_cast<uint16_t *>(out);
     a.ws = static_cast<unsigned char *>(workspace);
     OC_HIP(launch_attention(p, a, stream));

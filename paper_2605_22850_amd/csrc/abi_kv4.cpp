@@ -17,9 +17,6 @@ int check_kv4_layout(const oc_layout &l) {
     return OC_OK;
 }
 
-// page ids are 32-bit: those of a larger pool are all within it
-static int32_t pages_of(const oc_layout &l) { return (int32_t)std::min<int64_t>(l.num_pages, INT32_MAX); }
-
 static Kv4Args kv4_args(const oc_kv_pool *pool, const oc_block_table *bt, int32_t layer, int64_t first, int64_t tokens) {
     const oc_layout &l = pool->layout;
     Kv4Args a{};

@@ -48,7 +48,7 @@ struct KParams {
     float *o_part, *ml_part;
     uint16_t *out;
     int64_t Tp, Ts, rows, rows_pad, n_pre_pages, n_suf_pages, n_blocks, blocks_per_split;
-    int nq, nkv, grp, m_tiles, n_split, n_groups;
+    int nq, nkv, grp, m_tiles, n_split, n_groups, num_pages;
     float scale_log2;
 };
 
@@ -187,6 +187,12 @@ __global__ __launch_bounds__(THREADS) void attn_fwd_kernel(KBatch batch) {
     const int n_fast_pages = nkv * head_block * 2 <= 0xFFFFFFFFLL ? n_pre_pages : 0;
     const unsigned char *const kg = reinterpret_cast<const unsigned char *>(pool_k + g * head_block);
     const int64_t kv_step = (pool_v - pool_k) * 2;
+    // An id outside the pool (pages_of) reads the pool's last page.  One minimum, at the
+    // copy and not where the id is loaded, a block ahead, which would wait for it.  (A
+    // comparison and a choice of page 0 took 1 to 2 % at d = 64: 8/8 heads, 9968 + 2586
+    // tokens, 118.6 us like this, 121.5.)
+    const uint32_t pool_end = (uint32_t)p.num_pages - 1;
+    auto page_in = [&](int32_t id) { return min((uint32_t)id, pool_end); };
     auto issue_block = [&](int b, int buf, const int32_t (&pid)[CPW]) {
         uint16_t *kt_lds = lds + buf * 2 * TILE;
         uint16_t *vt_lds = kt_lds + TILE;
@@ -194,7 +200,7 @@ __global__ __launch_bounds__(THREADS) void attn_fwd_kernel(KBatch batch) {
 #pragma unroll
             for (int u = 0; u < CPW; ++u) {
                 const int q = u * WAVES + wave;
-                const unsigned char *kp = kg + (uint64_t)(uint32_t)pid[u] * page_bytes;
+                const unsigned char *kp = kg + (uint64_t)page_in(pid[u]) * page_bytes;
                 dma16(kp, klane[u], kt_lds + q * 512);
                 dma16(kp + kv_step, vlane[u], vt_lds + q * 512);
             }
@@ -205,7 +211,7 @@ __global__ __launch_bounds__(THREADS) void attn_fwd_kernel(KBatch batch) {
             const int q = u * WAVES + wave;                   // chunk index, uniform per wavefront
             const int v = b * 4 + q / CPP;                    // page of the key sequence
             if (v < n_pre_pages) {
-                const int64_t blk = ((int64_t)pid[u] * nkv + g) * head_block;
+                const int64_t blk = ((int64_t)page_in(pid[u]) * nkv + g) * head_block;
                 dma16(pool_k + blk, klane[u], kt_lds + q * 512);
                 dma16(pool_v + blk, vlane[u], vt_lds + q * 512);
             } else {
@@ -496,6 +502,12 @@ __global__ __launch_bounds__(NW * 64) void attn_ways_kernel(KParams p) {
             pid[h] = v < n_pre_pages ? pages_c[v] : 0;
         }
     };
+    // an id outside the pool reads its last page, as in the kernel above; apart from the
+    // load, which is not waited for there
+    auto keep_inside = [&](int32_t (&pid)[2]) {
+#pragma unroll
+        for (int h = 0; h < 2; ++h) pid[h] = (int32_t)min((uint32_t)pid[h], (uint32_t)p.num_pages - 1);
+    };
     // copy one unit's K (or V) rows: two pages of the pool, or suffix rows
     auto issue = [&](int j, const int32_t (&pid)[2], bool is_k, uint16_t *dst) {
         const uint16_t *const pool = is_k ? p.pool_k : p.pool_v, *const dense = is_k ? p.k_new : p.v_new;
@@ -543,6 +555,7 @@ __global__ __launch_bounds__(NW * 64) void attn_ways_kernel(KParams p) {
     int32_t pid[2];
     if (n > 0) {
         load_pids(0, pid);
+        keep_inside(pid);
         issue(0, pid, true, K);
         issue(0, pid, false, V);
     }
@@ -617,7 +630,10 @@ __global__ __launch_bounds__(NW * 64) void attn_ways_kernel(KParams p) {
             }
         }
         asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");      // K is read: its buffer may be refilled
-        if (refill) issue(j + 1, pid, true, K);
+        if (refill) {
+            keep_inside(pid);
+            issue(j + 1, pid, true, K);
+        }
 
         if ((u + 1) * 2 > full_pre_pages) {     // the prefix's partial last page, or suffix keys
             const int ps = n_pre_pages * PAGE - u * UNIT, pe = Tp - u * UNIT;
@@ -1034,6 +1050,7 @@ static KParams make_params(const AttnPlan &pl, const AttnArgs &a) {
     p.pool_k = a.pool_k;
     p.pool_v = a.pool_v;
     p.pages = a.pages;
+    p.num_pages = a.num_pages;
     p.k_new = a.k_new;
     p.v_new = a.v_new;
     p.o_part = reinterpret_cast<float *>(a.ws + pl.off_o);

@@ -3,6 +3,7 @@
 
 #include <hip/hip_runtime.h>
 
+#include <algorithm>
 #include <cstdint>
 #include <cstdio>
 #include <new>
@@ -64,6 +65,11 @@ int check_layout(const oc_layout &l);
 int check_table(const oc_block_table *bt, const oc_layout &l);
 int check_staging_shape(const oc_layout &l, const oc_block_table *bt, int64_t num_chunks, int64_t slice_bytes);
 
+// Pages that the kernels hold a table's 32-bit ids against: a table may hold ids
+// outside the pool (a fork or take that found no page leaves -1 on the device).  Nothing
+// is stored to or copied from such a page, and attention reads another in its place.
+inline int32_t pages_of(const oc_layout &l) { return (int32_t)std::min<int64_t>(l.num_pages, INT32_MAX); }
+
 // ---- ingest / gather ------------------------------------------------------
 struct IngestArgs {
     const uint16_t *staging;   // chunk slices [N][2][G][n_kv][d], chunk_stride apart
@@ -78,6 +84,7 @@ struct IngestArgs {
     // objects the layer count with the per-layer steps in staging and pool
     int64_t chunk_stride, token0;
     int32_t n_layers;
+    int32_t num_pages;         // ids outside [0, num_pages) name no page
     int64_t layer_step_staging, layer_step_pool;
     // filled by the launcher
     int64_t region;            // pool_v - pool_k, elements
@@ -106,7 +113,7 @@ struct AppendArgs {
     uint16_t *pool_k, *pool_v;       // the layer's K and V regions
     const int32_t *pages;
     int64_t num_tokens, token0;      // suffix tokens, the first one's logical position
-    int32_t n_kv, d, Ps;
+    int32_t n_kv, d, Ps, num_pages;
     // filled by the launcher
     int64_t region;
     int32_t d8, lg_d8, lg_nkv, lg_ps;
@@ -222,6 +229,7 @@ struct AttnArgs {
     const uint16_t *q, *k_new, *v_new;
     const uint16_t *pool_k, *pool_v;   // layer bases as in IngestArgs
     const int32_t *pages;
+    int32_t num_pages;
     uint16_t *out;
     unsigned char *ws;
 };

@@ -26,6 +26,18 @@ typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 
 constexpr int kThreads = 256;
 
+// Before a test of a page id: the payload's loads are in flight with the id's; the
+// compiler would sink them behind the test, which waits for the id.
+__device__ inline void loads_stay_here() { asm volatile("" ::: "memory"); }
+// ... and the address that the id gives is worked out, with what it takes of the
+// kernel's arguments, which it would fetch behind the test (chunk objects 1.3 % slower).
+template <class T>
+__device__ inline auto address_here(T *p) {
+    auto g = (__attribute__((address_space(1))) T *)p;
+    asm volatile("" : "+v"(g));
+    return g;
+}
+
 // 8 slots x one 16-byte column of one (page, head) block, K then V.  With
 // POW2 (d/8, page size, KV heads and a chunk size of at least 8 all powers of
 // two) the decode is shifts and masks and the 8 tokens sit in one chunk.
@@ -59,6 +71,7 @@ __global__ __launch_bounds__(kThreads, 8) void kv_ingest_rows_kernel(IngestArgs 
     if (left <= 0) return;                               // slots past the prefix
     const int64_t D = (int64_t)nkv * d;
     const int64_t page = a.pages[q];
+    const bool there = (uint32_t)page < (uint32_t)a.num_pages;   // else no page of the pool
     uint16_t *kdst = a.pool_k + ((page * nkv + h) * a.Ps + s8 * 8) * (int64_t)d + c * 8;
     const int64_t col = (int64_t)h * d + c * 8;
     const int64_t vstep = (int64_t)G * D;                // K row -> V row of a token
@@ -76,6 +89,10 @@ __global__ __launch_bounds__(kThreads, 8) void kv_ingest_rows_kernel(IngestArgs 
 #pragma unroll
             for (int i = 0; i < 8; ++i)
                 r[i] = __builtin_nontemporal_load(reinterpret_cast<const u32x4 *>(src + kv * vstep + i * D));
+            if (kv == 0) {
+                loads_stay_here();
+                if (!there) return;
+            }
 #pragma unroll
             for (int i = 0; i < 8; ++i)
                 __builtin_nontemporal_store(r[i], reinterpret_cast<u32x4 *>(kdst + kv * a.region + i * d));
@@ -97,6 +114,10 @@ __global__ __launch_bounds__(kThreads, 8) void kv_ingest_rows_kernel(IngestArgs 
         for (int i = 0; i < 8; ++i)
             if (i < valid)
                 r[i] = __builtin_nontemporal_load(reinterpret_cast<const u32x4 *>(a.staging + src[i] + kv * vstep));
+        if (kv == 0) {
+            loads_stay_here();
+            if (!there) return;
+        }
 #pragma unroll
         for (int i = 0; i < 8; ++i)
             if (i < valid) __builtin_nontemporal_store(r[i], reinterpret_cast<u32x4 *>(kdst + kv * a.region + i * d));
@@ -106,10 +127,13 @@ __global__ __launch_bounds__(kThreads, 8) void kv_ingest_rows_kernel(IngestArgs 
 // Piece e of a payload numbered in payload order ([chunk][K|V][token][head]
 // [16-byte column]; from chunk blockIdx.z on) -> its element offsets in the
 // staging (from `staging`) and in the pool (from `pool_k`), both including the
-// layer step of blockIdx.y.  With POW2 every divisor (d/8, KV heads, chunk size, page size)
-// is a power of two and the decode is shifts and masks.
+// layer step of blockIdx.y; false, and a place in page 0, where the table names no page
+// of the pool (the gather loads from there and stores nothing: a load that waited for
+// the test took 1 % longer over whole objects).  With POW2
+// every divisor (d/8, KV heads, chunk size, page size) is a power of two and the decode
+// is shifts and masks.
 template <bool POW2>
-__device__ inline void src_order_piece(const IngestArgs &a, int64_t e, int64_t &stage, int64_t &pool) {
+__device__ inline bool src_order_piece(const IngestArgs &a, int64_t e, int64_t &stage, int64_t &pool) {
     const int64_t slice_pieces = 2LL * a.G * a.n_kv * a.d8;   // 16-byte pieces per chunk slice
     int c, h, t, kv;
     int64_t j;
@@ -139,10 +163,13 @@ __device__ inline void src_order_piece(const IngestArgs &a, int64_t e, int64_t &
         q = T / a.Ps;
         slot = T - q * a.Ps;
     }
-    const int64_t page = a.pages[q];
+    int32_t page = a.pages[q];
+    const bool there = (uint32_t)page < (uint32_t)a.num_pages;
+    page = there ? page : 0;
     stage = blockIdx.y * a.layer_step_staging + jz * a.chunk_stride + (e - j * slice_pieces) * 8;
-    pool = blockIdx.y * a.layer_step_pool + kv * a.region + ((page * a.n_kv + h) * a.Ps + slot) * (int64_t)a.d +
+    pool = blockIdx.y * a.layer_step_pool + kv * a.region + (((int64_t)page * a.n_kv + h) * a.Ps + slot) * a.d +
            c * 8;
+    return there;
 }
 
 // Ingest, one 16-byte piece per thread in payload order: every wavefront
@@ -157,9 +184,11 @@ __global__ __launch_bounds__(kThreads) void kv_ingest_src_kernel(IngestArgs a, i
     const int64_t e = (int64_t)blockIdx.x * kThreads + threadIdx.x;
     if (e >= n_pieces) return;
     int64_t stage, pool;
-    src_order_piece<POW2>(a, e, stage, pool);
+    const bool there = src_order_piece<POW2>(a, e, stage, pool);
     const u32x4 v = __builtin_nontemporal_load(reinterpret_cast<const u32x4 *>(a.staging + stage));
-    __builtin_nontemporal_store(v, reinterpret_cast<u32x4 *>(a.pool_k + pool));
+    loads_stay_here();
+    auto *const to = address_here(reinterpret_cast<u32x4 *>(a.pool_k + pool));
+    if (there) __builtin_nontemporal_store(v, to);
 }
 
 // Gather (pool -> layer payload or whole chunk objects, the offload
@@ -172,9 +201,11 @@ __global__ __launch_bounds__(kThreads) void kv_gather_src_kernel(IngestArgs a, u
     const int64_t e = (int64_t)blockIdx.x * kThreads + threadIdx.x;
     if (e >= n_pieces) return;
     int64_t stage, pool;
-    src_order_piece<POW2>(a, e, stage, pool);
+    const bool there = src_order_piece<POW2>(a, e, stage, pool);
     const u32x4 v = __builtin_nontemporal_load(reinterpret_cast<const u32x4 *>(a.pool_k + pool));
-    __builtin_nontemporal_store(v, reinterpret_cast<u32x4 *>(out + stage));
+    loads_stay_here();
+    auto *const to = address_here(reinterpret_cast<u32x4 *>(out + stage));
+    if (there) __builtin_nontemporal_store(v, to);
 }
 
 // Suffix append: token i of k_new / v_new ([T_s][n_kv][d]; blockIdx.y picks
@@ -204,8 +235,10 @@ __device__ inline void append_piece(const Args &a, uint32_t e, int kv) {
     const uint16_t *src = (kv ? a.v_new : a.k_new) + (int64_t)e * 8;
     const u32x4 v = *reinterpret_cast<const u32x4 *>(src);
     const int64_t page = a.pages[q];
+    loads_stay_here();
     uint16_t *dst = a.pool_k + kv * a.region + ((page * a.n_kv + h) * a.Ps + slot) * (int64_t)a.d + c * 8;
-    *reinterpret_cast<u32x4 *>(dst) = v;
+    auto *const to = address_here(reinterpret_cast<u32x4 *>(dst));
+    if ((uint32_t)page < (uint32_t)a.num_pages) *to = v;     // else no page of the pool
 }
 
 // One layer's suffix is a few MiB, so this is launch and latency bound (4 MiB

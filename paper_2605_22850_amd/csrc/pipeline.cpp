@@ -851,6 +851,7 @@ static int run_pipeline(Context *c, const oc_request *reqs, int32_t n_reqs, oc_r
         a.pool_k = base + ((int64_t)layer * 2 + 0) * l.num_pages * block;
         a.pool_v = base + ((int64_t)layer * 2 + 1) * l.num_pages * block;
         a.pages = r.block_table->pages;
+        a.num_pages = pages_of(l);
         a.ws = ws;
         return a;
     };
@@ -1202,6 +1203,7 @@ static int run_pipeline(Context *c, const oc_request *reqs, int32_t n_reqs, oc_r
                 a.n_kv = l.num_kv_heads;
                 a.d = l.head_dim;
                 a.Ps = l.page_size;
+                a.num_pages = pages_of(l);
                 // beside an attention: past the first item; batched, past the
                 // first layer, whose attention waits for all its ingests
                 const bool beside = batched ? it.layer > 0 : step > 0;
