@@ -231,6 +231,8 @@ __global__ __launch_bounds__(THREADS) void attn_fwd_kernel(KBatch batch) {
     for (int et = 0; et < D / 32; ++et) w.o[et] = f32x16{};
     w.m = -__builtin_inff();
     w.l = 0.f;
+    w.scale = scale_log2;
+    w.m_use = 0.f;
     const int krow = key_perm(col);
     int voff[D / 32];
 #pragma unroll
@@ -660,9 +662,11 @@ __global__ __launch_bounds__(NW * 64) void attn_ways_kernel(KParams p) {
             float mx[2] = {-__builtin_inff(), -__builtin_inff()};
 #pragma unroll
             for (int i = 0; i < 16; ++i) mx[i & 1] = fmaxf(mx[i & 1], s[qb][i]);
-            const float mu = half_swap_max(fmaxf(mx[0], mx[1])) * scale_log2;
-            if (__any(mu > m[qb] + RESCALE_SLACK)) {
-                const float mn = fmaxf(m[qb], mu);
+            const float top = half_swap_max(fmaxf(mx[0], mx[1]));
+            float scale = row_scale(m[qb], scale_log2);
+            if (__any(top * scale > m[qb] + RESCALE_SLACK)) {
+                const float mn = raise_row(m[qb], scale, top, scale_log2);
+                scale = row_scale(mn, scale_log2);
                 const float alpha = __builtin_amdgcn_exp2f(m[qb] - (mn == -__builtin_inff() ? 0.f : mn));
                 m[qb] = mn;
                 l[qb] *= alpha;
@@ -678,7 +682,7 @@ __global__ __launch_bounds__(NW * 64) void attn_ways_kernel(KParams p) {
                 f32x8 e;
 #pragma unroll
                 for (int i = 0; i < 8; ++i)
-                    e[i] = __builtin_amdgcn_exp2f(fmaf(s[qb][hf * 8 + i], scale_log2, -m_use));
+                    e[i] = __builtin_amdgcn_exp2f(fmaf(s[qb][hf * 8 + i], scale, -m_use));
                 const bf16x8 b = __builtin_convertvector(e, bf16x8);
                 pp[qb][hf] = b;
                 ls[0] = __builtin_amdgcn_fdot2_f32_bf16(__builtin_shufflevector(b, b, 0, 1), ones, ls[0], false);

@@ -17,6 +17,26 @@ constexpr int THREADS = WAVES * 64;
 constexpr float RESCALE_SLACK = 8.0f;   // log2 units the running max may lag
 constexpr int LOOKAHEAD = 3;              // MFMAs an operand read runs ahead of its use
 
+// A row's P is 2^(s * scale - m), the product unrounded (one fma), and m the rounded
+// product of its largest score (log2 units).  All of its P are thus off by one factor
+// 2^r, r half a step of m at most, which the row's sum takes out again; but past |m| =
+// 2^31 r is more than an exponent holds, and P and sum would all be infinite or 0.
+// So each row has a scale of its own, and a row whose largest score is 2^31 or more (m
+// past 2^28, r 8) takes 1/4, with which every product is exact.  It need not be the
+// right one: two fp32 scores there differ by 2^16 in P or not at all, and with either
+// scale the smaller one vanishes.  It is larger than any other (log2(e) / 8 at d = 64),
+// so that where such a row meets a part of itself with smaller scores, in another
+// wavefront or split, the larger score has the larger m.
+constexpr float LARGE_SCORE = 0x1p31f, LARGE_SCALE = 0.25f, LARGE_M = LARGE_SCORE * LARGE_SCALE;
+// of a row with running maximum m (-inf, a row without a key, has no P that it matters to)
+__device__ __forceinline__ float row_scale(float m, float scale_log2) {
+    return __builtin_fabsf(m) >= LARGE_M ? LARGE_SCALE : scale_log2;
+}
+// the running maximum of a row after scores of at most `top`
+__device__ __forceinline__ float raise_row(float m, float scale, float top, float scale_log2) {
+    return top * scale > m ? top * (__builtin_fabsf(top) >= LARGE_SCORE ? LARGE_SCALE : scale_log2) : m;
+}
+
 // value of the lane 32 positions away (the other half of the wavefront)
 __device__ inline float half_swap_max(float x) {
     auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
@@ -73,7 +93,8 @@ struct WaveState {
     f32x16 o[D / 32];    // O^T: 32 dims x 32 rows per tile, fp32
     f32x16 s[2];         // scores of the current block, one 32-key half each
     bf16x8 p[2][2];      // P of the last softmaxed block as the PV operand: [half][8-key group]
-    float m, l;          // running maximum (log2 units) and sum of this lane's row
+    float scale, m_use;  // this lane's row: row_scale(), and m, or 0 while that is -inf
+    float m, l;          // its running maximum (log2 units) and sum
 };
 
 // The first LOOKAHEAD V^T fragments of a PV pass, read ahead of the barrier
@@ -139,16 +160,17 @@ __device__ __forceinline__ void softmax_phase(WaveState<D> &w, float scale_log2)
     for (int kt = 0; kt < 2; ++kt)
 #pragma unroll
         for (int i2 = 0; i2 < 16; ++i2) mx[i2 & 1] = fmaxf(mx[i2 & 1], w.s[kt][i2]);
-    const float mblk = half_swap_max(fmaxf(mx[0], mx[1])) * scale_log2;
-    if (__any(mblk > w.m + RESCALE_SLACK)) {
-        const float m_new = fmaxf(w.m, mblk);
+    const float top = half_swap_max(fmaxf(mx[0], mx[1]));
+    if (__any(top * w.scale > w.m + RESCALE_SLACK)) {
+        const float m_new = raise_row(w.m, w.scale, top, scale_log2);
+        w.scale = row_scale(m_new, scale_log2);
+        w.m_use = m_new == -__builtin_inff() ? 0.f : m_new;
         const float alpha = __builtin_amdgcn_exp2f(w.m - (m_new == -__builtin_inff() ? 0.f : m_new));
         w.m = m_new;
         w.l *= alpha;
 #pragma unroll
         for (int et = 0; et < D / 32; ++et) w.o[et] *= alpha;
     }
-    const float m_use = w.m == -__builtin_inff() ? 0.f : w.m;
     // row sums of the rounded P (the values the PV product uses), two bf16
     // pairs per dot instruction, two partial sums
     typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
@@ -161,7 +183,7 @@ __device__ __forceinline__ void softmax_phase(WaveState<D> &w, float scale_log2)
             f32x8 pv;
 #pragma unroll
             for (int i2 = 0; i2 < 8; ++i2)
-                pv[i2] = __builtin_amdgcn_exp2f(fmaf(w.s[kt][hf * 8 + i2], scale_log2, -m_use));
+                pv[i2] = __builtin_amdgcn_exp2f(fmaf(w.s[kt][hf * 8 + i2], w.scale, -w.m_use));
             const bf16x8 pp = __builtin_convertvector(pv, bf16x8);
             w.p[kt][hf] = pp;
             lsum[0] = __builtin_amdgcn_fdot2_f32_bf16(__builtin_shufflevector(pp, pp, 0, 1), ones, lsum[0], false);

@@ -300,9 +300,10 @@ __global__ __launch_bounds__(NW4 * 64, NR == 1 ? 4 : 2) void kv4_ways_kernel(Kv4
     const int tok0 = mt * ROWS / grp;
 
     f32x4 o[NR][NT];
-    float m[NR], l[NR];
+    float m[NR], l[NR], scale[NR];
 #pragma unroll
     for (int r = 0; r < NR; ++r) {
+        scale[r] = scale_log2;
         m[r] = -__builtin_inff();
         l[r] = 0.f;
 #pragma unroll
@@ -322,10 +323,11 @@ __global__ __launch_bounds__(NW4 * 64, NR == 1 ? 4 : 2) void kv4_ways_kernel(Kv4
             float mx[2];
 #pragma unroll
             for (int i = 0; i < 2; ++i) mx[i] = max2(max2(s[r][i][0], s[r][i][1]), max2(s[r][i][2], s[r][i][3]));
-            const float mu = max2(mx[0], mx[1]) * scale_log2;
+            const float top = max2(mx[0], mx[1]);
             // the running maximum is raised, and O rescaled, only when a score exceeds it by 2^RESCALE_SLACK
-            if (__any(mu > m[r] + RESCALE_SLACK)) {
-                const float mn = fmaxf(m[r], row_max(mu));
+            if (__any(top * scale[r] > m[r] + RESCALE_SLACK)) {
+                const float mn = raise_row(m[r], scale[r], row_max(top), scale_log2);
+                scale[r] = row_scale(mn, scale_log2);
                 const float alpha = __builtin_amdgcn_exp2f(m[r] - (mn == -__builtin_inff() ? 0.f : mn));
                 m[r] = mn;
                 l[r] *= alpha;
@@ -335,7 +337,7 @@ __global__ __launch_bounds__(NW4 * 64, NR == 1 ? 4 : 2) void kv4_ways_kernel(Kv4
             const float m_use = m[r] == -__builtin_inff() ? 0.f : m[r];
             f32x8 e;
 #pragma unroll
-            for (int i = 0; i < 8; ++i) e[i] = __builtin_amdgcn_exp2f(fmaf(s[r][i >> 2][i & 3], scale_log2, -m_use));
+            for (int i = 0; i < 8; ++i) e[i] = __builtin_amdgcn_exp2f(fmaf(s[r][i >> 2][i & 3], scale[r], -m_use));
             // bfloat16 P for the matrix cores; the sum is over the rounded values that the product uses
             const bf16x8 bp = __builtin_convertvector(e, bf16x8);
             pp[r] = bp;
@@ -726,6 +728,8 @@ __global__ __launch_bounds__(THREADS) void kv4_rows_kernel(Kv4Params p) {
     for (int et = 0; et < D / 32; ++et) w.o[et] = f32x16{};
     w.m = -__builtin_inff();
     w.l = 0.f;
+    w.scale = scale_log2;
+    w.m_use = 0.f;
     const int krow = key_perm(col);
     int voff[D / 32];
 #pragma unroll
