@@ -1143,7 +1143,7 @@ int plan_kv4_decode(const oc_layout &l, int64_t batch, int64_t max_tokens, Kv4Pl
     p.m_tiles = (int)((p.rows + p.row_tile - 1) / p.row_tile);
     p.n_units = (int)(((max_tokens + PAGE - 1) / PAGE + 1) / 2);
     const int64_t pairs = batch * p.nkv;
-    if (p.m_tiles > 65535) return fail(OC_ERANGE, "more than 2^20 query heads to a KV head");
+    if (p.m_tiles > 65535) return fail(OC_ERANGE, "more than 65535 * 32 query heads to a KV head");
     const int64_t most = OC_MAX_GRID_ITEMS / THREADS / p.nkv;       // ranges a grid can have
     const int64_t fill = 256 / (pairs * p.m_tiles);                // ranges of each pair that fill the CUs
     int64_t n_ranges = batch;
