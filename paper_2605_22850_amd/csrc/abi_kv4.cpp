@@ -8,13 +8,19 @@
 
 namespace oc {
 
+// pages of K and of V in every layer, whose byte offsets are 64-bit
+static int check_pool_bytes(const oc_layout &l, int64_t page_bytes) {
+    if (l.num_pages > INT64_MAX / 2 / l.num_layers / page_bytes) return fail(OC_ERANGE, "a pool of more than 2^63 bytes");
+    return OC_OK;
+}
+
 int check_kv4_layout(const oc_layout &l) {
     const int rc = check_layout(l);
     if (rc) return rc;
     if (l.head_dim % 32) return fail(OC_ESHAPE, "a 4-bit pool needs a head_dim that is a multiple of 32");
     if ((int64_t)l.page_size * l.head_dim > INT32_MAX || kv4_page_bytes(l) > INT32_MAX)
         return fail(OC_ERANGE, "a 4-bit page of 2^31 bytes or more");
-    return OC_OK;
+    return check_pool_bytes(l, kv4_page_bytes(l));
 }
 
 static Kv4Args kv4_args(const oc_kv_pool *pool, const oc_block_table *bt, int32_t layer, int64_t first, int64_t tokens) {
@@ -221,8 +227,11 @@ static int pages_args(const oc_kv_pool *pool, int32_t bits, PagesArgs *a) {
     if (rc) return rc;
     if (bits != 16 && bits != 4) return fail(OC_EINVAL, "bits must be 16 or 4");
     if (bits == 4 && (rc = check_kv4_layout(l))) return rc;
+    if (bits == 16 && (int64_t)l.num_kv_heads * l.page_size > INT64_MAX / 2 / l.head_dim)
+        return fail(OC_ERANGE, "a page of more than 2^63 bytes");
     *a = PagesArgs{};
     a->page_bytes = bits == 4 ? kv4_page_bytes(l) : (int64_t)l.num_kv_heads * l.page_size * l.head_dim * 2;
+    if ((rc = check_pool_bytes(l, a->page_bytes))) return rc;
     a->pool = static_cast<unsigned char *>(pool->base);
     a->regions = 2 * l.num_layers;
     a->num_pages = (int32_t)l.num_pages;
@@ -354,9 +363,6 @@ extern "C" {
 size_t oc_kv4_pool_bytes(const oc_layout *layout) {
     return bytes_of(layout, [&](size_t *n) {
         const int rc = check_kv4_layout(*layout);
-        // 2 * L * P pages of less than 2^31 bytes
-        if (!rc && layout->num_pages > INT64_MAX / 2 / layout->num_layers / kv4_page_bytes(*layout))
-            return fail(OC_ERANGE, "a pool of more than 2^63 bytes");
         *n = rc ? 0 : (size_t)(2 * layout->num_layers * layout->num_pages * kv4_page_bytes(*layout));
         return rc;
     });
