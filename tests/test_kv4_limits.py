@@ -29,7 +29,7 @@ def test_pools_whose_offsets_have_no_64_bit_number():
                  lambda: lib.oc_kv4_suffix_prefill_layer(far, far, far, 3, ref(kp), ref(bt), 1 << 19, far, far, 1 << 30, None),
                  lambda: lib.oc_kv4_decode_layer(far, far, far, 1, ref(kp), ref(tabs), far, 32, 1 << 19, far, far, 1 << 30, None)):
         assert call() == L.OC_ERANGE and b"2^63" in lib.oc_last_error()
-    for shape in ((1 << 30, 1, 1, 1 << 20, 16, 16, (1 << 31) - 1), (1, 1 << 30, 1 << 30, 1 << 20, 1 << 20, 16, 64),
+    for shape in ((1 << 29, 1, 1, 1 << 20, 16, 16, (1 << 31) - 1), (1, 1 << 30, 1 << 30, 1 << 20, 1 << 20, 16, 64),
                   (1, 1 << 30, 1 << 30, 1 << 30, 8, 16, 64)):
         kp = L.c_kv_pool(far, L.c_layout(*shape))
         for call in (lambda: lib.oc_kv_pages_copy(ref(kp), 16, far, far, 2, None),
