@@ -343,7 +343,10 @@ size_t oc_kv4_decode_workspace_bytes(const oc_layout *layout, int64_t batch, int
  * bfloat16, 16-byte aligned.  num_tokens is DEVICE int32 [batch]: a captured
  * call can be replayed as the requests grow; the caller adds 1 after the last
  * layer.  num_tokens[i] < 0 marks an empty place: nothing of it is read or
- * written.  Lengths above max_tokens are taken as max_tokens.  Every table needs
+ * written.  Lengths above max_tokens are taken as max_tokens, so that the new token
+ * replaces the one cached at position max_tokens: before a request outgrows the
+ * max_tokens that a captured call was given, its place has to be emptied (-1) or the
+ * call captured anew.  Every table needs
  * max_tokens / page_size + 1 entries, of which the first
  * num_tokens[i] / page_size + 1 are used; the page that receives the token must
  * be no other table's (oc_kv_pages_fork sees to that).  An id outside [0, P), as

@@ -45,12 +45,16 @@ struct Kv4Params {
 // What bounds it, and measured: decode by its codes and scales from memory (eight
 // requests of 32K tokens at 64/8/128: 272 MB in 48.5 us, 5.6 TB/s; 30 of 0 to 28560 at
 // 32/8/128: 210 MB in 42.6, 4.9 TB/s; matrix units 10 % busy, vector units 30 %).  One new
-// token over 32763: 35.7 MB in 9.1 us and a merge of 2.6.  At 128 new tokens over
-// 4096 two workgroups of each CU do a chain of four dependent rounds per wavefront (load,
-// product, softmax, LDS, product): 22 us in all, where its products alone are 7 at the
-// rate of a large one.  Sixteen wavefronts to a workgroup, two or three units ahead, and
-// the next unit's scores before this one's softmax did not shorten it; 64-row tiles with
-// Q in LDS gained at one shape of the 75 below (512 tokens over 1024).
+// token over 32763: 35.7 MB in 9.7 us (10.4 where they are not in the last cache) and a
+// merge of 2.8; its 1025 units in 32 splits are 33 each, so that one wavefront of each
+// workgroup has a fifth round.  At 128 new tokens over 4096 there is one workgroup to a CU,
+// whose eight wavefronts have 16 or 17 units each: 22 us, where the products alone are 7
+// at the rate of a large one (matrix units 11 % busy, vector units 33, LDS 28).  Each of a
+// head's 32 row tiles reads and decodes all of its keys; by the rule's constants below
+// that is 17 us for a workgroup's 132 units, and the chain of 17 dependent rounds (load,
+// product, softmax, LDS, product) takes 10.  Sixteen wavefronts to a workgroup, two or three
+// units ahead, and the next unit's scores before this one's softmax did not shorten it;
+// 64-row tiles with Q in LDS gained at one shape of the 75 below (512 tokens over 1024).
 // ---------------------------------------------------------------------------
 
 // XOR on the 16-byte column of V row r (key in its page).  The columns of eight
@@ -60,10 +64,12 @@ struct Kv4Params {
 // unit of one row tile, not 99.)
 __device__ __forceinline__ int v4_swz(int r) { return ((r & 3) << 1) | ((r >> 2) & 1); }
 
-// Codes and scale byte of this lane's quarter of its key's row, K's or V's.  ONCE:
-// nothing else reads the page, so its codes bypass the caches (decode of eight requests
-// of 32K tokens: 58 -> 52.5 us; a lone request's 35 MB, which a benchmark finds in the
-// caches again, gains nothing).
+// Codes and scale byte of this lane's quarter of its key's row, K's or V's.  ONCE (the
+// decode form): the codes bypass the caches, since as a rule nothing else reads the page
+// in the launch (decode of eight requests of 32K tokens: 58 -> 52.5 us; a lone request's
+// 35 MB, which a benchmark finds in the caches again, gains nothing).  Where something
+// does, it reads them again: requests that share a prefix, and the further row tiles of
+// more than 32 query heads to a KV head.
 template <int D>
 struct Piece4 {
     uint32_t c[D / 32], b;
